@@ -344,6 +344,144 @@ SLORR_API slorr_status_t slorr_plan_get_launches(slorr_plan_t plan, int32_t *ops
  * Either array may be NULL. Host only. */
 SLORR_API slorr_status_t slorr_plan_get_kernels(slorr_plan_t plan, const char **names, double *alg_flops);
 
+/* ------------------------------------------------------------------------
+ * Operators of a regularised block
+ *
+ * Most of the weights that the regularizer works on in a language model are the
+ * projections of its gated feed-forward blocks (App. F). The calls below run
+ * such a block in training and generation: the gated feed-forward itself, the
+ * join that ends it (the norm after the block, gate, residual scale, residual
+ * dropout and the norm before the next block) and dropout on its own.
+ *
+ * Tensors are row-major device buffers of the call's dtype (F32 or BF16). Every
+ * pointer is 16-byte aligned. Sums, norms and activations are formed in fp32;
+ * every output is rounded once, to nearest even. The calls keep no state of
+ * their own: no plan, no cache, no allocation, nothing read back to the host;
+ * they can be captured into a graph. Results are the same bit for bit from call
+ * to call. Outputs must not overlap inputs or each other unless said otherwise.
+ * ------------------------------------------------------------------------ */
+
+/* Activation of the gate projection. GELU: a Phi(a); GELU_TANH: its tanh form
+ * 0.5 a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))). */
+typedef enum { SLORR_SILU = 0, SLORR_GELU = 1, SLORR_GELU_TANH = 2 } slorr_act_t;
+
+/* A gated feed-forward block: y = h Wd^T, h = act(a) * b, a = x Wg^T, b = x Wu^T
+ * with Wg, Wu (inner x dim) and Wd (dim x inner) contiguous.
+ * 0 <= tokens < 2^31 - 1024, 1 <= dim, inner <= 2^20, strides below 2^22, and
+ * tokens * max(dim, inner) below about 2^43. */
+typedef struct {
+  int64_t tokens;        /* rows of x and y                                    */
+  int32_t dim, inner;
+  slorr_dtype_t dtype;   /* of every tensor                                    */
+  slorr_act_t act;
+  int64_t ldx, lddy;     /* elements from one row of x (of dy) to the next, at
+                            least dim; 0 -> dim. y and dx are contiguous       */
+} slorr_ffn_t;
+
+/* Bytes of the buffers that the calls below need for this block: `state`, which
+ * carries a and b from a forward call to its backward (F32: as fp32; BF16: as
+ * 16-bit integers with one power of two per 8 consecutive values, so to 2^-16 of
+ * the largest of the eight), and the workspaces of the two calls. Never 0. Host only; any pointer may be NULL. */
+SLORR_API slorr_status_t slorr_ffn_sizes(const slorr_ffn_t *block, size_t *state_bytes,
+                                 size_t *forward_bytes, size_t *backward_bytes);
+
+/* Forward. state: 16-byte aligned, or NULL where no backward follows.
+ * workspace: 256-byte aligned, workspace_bytes at least slorr_ffn_sizes'. In
+ * BF16, h is rounded to bf16 before its product with Wd. F32 products are sums
+ * of six bf16 products that together carry fp32's 24 bits; an infinity in an
+ * F32 operand gives NaN. tokens == 0 writes nothing.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED (dtype, act, limits), WORKSPACE, HIP. */
+SLORR_API slorr_status_t slorr_ffn_forward(const slorr_ffn_t *block, const void *x, const void *w_gate,
+                                 const void *w_up, const void *w_down, void *y, void *state,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* Backward: the gradients of sum(dy * y) for x and the three weights, from the
+ * state that the forward call of the same block, x and weights wrote. Each of
+ * dx (tokens x dim), dw_gate, dw_up (inner x dim) and dw_down (dim x inner) is
+ * written, contiguous, or skipped where it is NULL. In BF16, h and the
+ * gradients of a and b are rounded to bf16 before their products. tokens == 0
+ * writes zero weight gradients. The call reads state and changes nothing in it. */
+SLORR_API slorr_status_t slorr_ffn_backward(const slorr_ffn_t *block, const void *dy, const void *x,
+                                 const void *w_gate, const void *w_up, const void *w_down,
+                                 const void *state, void *dx, void *dw_gate, void *dw_up,
+                                 void *dw_down, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Norm over a row t of dim values: RMS t / sqrt(mean(t^2) + eps); LAYER
+ * (t - mean(t)) / sqrt(var(t) + eps) with the biased variance. */
+typedef enum { SLORR_RMS = 0, SLORR_LAYER = 1 } slorr_norm_t;
+
+#define SLORR_JOIN_POST 0x1u     /* norm of f (post_weight, post_bias)                    */
+#define SLORR_JOIN_PRE  0x2u     /* norm of y (pre_weight, pre_bias): the output z        */
+
+/* The join between two blocks, over rows of dim values:
+ *
+ *   u = norm(f) * post_weight + post_bias      (POST; else u = f)
+ *   y = x + alpha * scale * gate * drop(u)
+ *   z = norm(y) * pre_weight + pre_bias        (PRE; of y before its rounding)
+ *
+ * x is the residual stream, f the block's output. Without f (NULL) y is x and
+ * the call is the norm alone. drop is slorr_dropout with the element index
+ * row * dim + column. 1 <= dim <= 8192, rows >= 0. */
+typedef struct {
+  int64_t rows;
+  int32_t dim;
+  slorr_dtype_t dtype;   /* of every tensor                                           */
+  slorr_norm_t norm;     /* of both norms                                             */
+  uint32_t flags;        /* SLORR_JOIN_*                                              */
+  int64_t gate_rows;     /* rows of gate: it divides rows, and gate row i belongs to the
+                            i-th run of rows / gate_rows rows (1: one for all, rows: one
+                            each); ignored without gate                               */
+  int64_t ldx, ldf, ld_gate;  /* elements from one row to the next, at least dim; 0 -> dim */
+  float eps;             /* >= 0 and finite                                           */
+  float alpha;           /* finite                                                    */
+  double p;              /* dropout rate, see slorr_dropout; 0: none                  */
+  int64_t site;
+} slorr_join_t;
+
+/* Inputs of a join. NULL: f (see above), gate and scale (taken as 1), biases
+ * (0), weights (1); a norm that the flags leave out must have no weight or bias. */
+typedef struct {
+  const void *x, *f;
+  const void *post_weight, *post_bias, *gate, *scale, *pre_weight, *pre_bias;
+} slorr_join_tensors_t;
+
+/* Gradients of a join's inputs, contiguous (gate: gate_rows x dim); NULL skips
+ * one. Those of an input that is NULL must be NULL. */
+typedef struct {
+  void *x, *f;
+  void *post_weight, *post_bias, *gate, *scale, *pre_weight, *pre_bias;
+} slorr_join_grads_t;
+
+/* Forward: y and z (contiguous). y may be NULL where PRE is set and f is NULL.
+ * rng: as in slorr_dropout; may be NULL with p == 0. */
+SLORR_API slorr_status_t slorr_join_forward(const slorr_join_t *join, const slorr_join_tensors_t *in,
+                                 const int64_t *rng, void *y, void *z, void *stream);
+
+/* Device workspace of slorr_join_backward, never 0. Host only. */
+SLORR_API slorr_status_t slorr_join_workspace(const slorr_join_t *join, size_t *bytes);
+
+/* Backward: the gradients of sum(dy * y) + sum(dz * z), dy and dz contiguous, either
+ * NULL where it is zero. It needs the forward call's inputs and rng values and
+ * nothing else: the norms are formed again. The sums over rows are in fp32 in a
+ * fixed order. rows == 0 writes zero gradients of the vectors. */
+SLORR_API slorr_status_t slorr_join_backward(const slorr_join_t *join, const slorr_join_tensors_t *in,
+                                 const int64_t *rng, const void *dy, const void *dz,
+                                 const slorr_join_grads_t *grads, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
+/* Dropout of n contiguous values: y_e = x_e / (1 - p') where element e is kept,
+ * else 0, with no mask in memory: calling it on dy gives the backward pass.
+ * Element e is kept where the 16-bit number e mod 8 (low half of word 0, high
+ * half of word 0, low half of word 1, ...) of the block
+ * Philox4x32-10(counter = (e div 8, rng[1] + site), key = rng[0]) (64-bit numbers,
+ * low word first; Salmon et al., "Parallel random numbers: as easy as 1, 2, 3")
+ * is at least t = round(2^16 p), and p' = t / 2^16, so the expected value is x
+ * exactly; 0 <= p, t < 2^16. rng: two int64 on the device, 8-byte aligned, read when
+ * the kernel runs, so a replayed graph draws anew when they change; site sets
+ * calls of one rng apart. y may be x. p' == 0 copies. */
+SLORR_API slorr_status_t slorr_dropout(int64_t n, slorr_dtype_t dtype, double p, const int64_t *rng,
+                                 int64_t site, const void *x, void *y, void *stream);
+
 /* Name of a status code (static string). */
 SLORR_API const char *slorr_status_string(slorr_status_t status);
 

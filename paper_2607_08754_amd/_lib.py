@@ -31,6 +31,11 @@ NO_GRAPH = 0x4
 AUX = 0x8
 DEFER_GRAD = 0x10
 
+# operators of a regularised block
+SILU, GELU, GELU_TANH = 0, 1, 2
+RMS, LAYER = 0, 1
+JOIN_POST, JOIN_PRE = 0x1, 0x2
+
 OPS = ("sumsq", "norm", "prep", "gram", "poly", "update", "last", "finalize", "grad", "setsum", "gram_reduce")
 
 EXPORTED = ("slorr_default_options", "slorr_pe_coefficients", "slorr_plan", "slorr_cache_config",
@@ -39,7 +44,9 @@ EXPORTED = ("slorr_default_options", "slorr_pe_coefficients", "slorr_plan", "slo
             "slorr_reg_fwd_bwd_profiled", "slorr_reg_fwd_bwd_noalloc",
             "slorr_plan_destroy", "slorr_plan_get_info", "slorr_plan_get_launches",
             "slorr_plan_get_kernels", "slorr_status_string",
-            "slorr_last_error")
+            "slorr_last_error",
+            "slorr_ffn_sizes", "slorr_ffn_forward", "slorr_ffn_backward",
+            "slorr_join_forward", "slorr_join_workspace", "slorr_join_backward", "slorr_dropout")
 
 
 class Shape(ctypes.Structure):
@@ -57,6 +64,23 @@ class PlanInfo(ctypes.Structure):
                 ("launches", ctypes.c_int32), ("gemm_tiles", ctypes.c_int64),
                 ("paper_flops", ctypes.c_double), ("mfma_flops", ctypes.c_double),
                 ("weight_bytes", ctypes.c_double), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class Ffn(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("dim", ctypes.c_int32), ("inner", ctypes.c_int32),
+                ("dtype", ctypes.c_int), ("act", ctypes.c_int), ("ldx", ctypes.c_int64), ("lddy", ctypes.c_int64)]
+
+
+class Join(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("norm", ctypes.c_int),
+                ("flags", ctypes.c_uint32), ("gate_rows", ctypes.c_int64), ("ldx", ctypes.c_int64),
+                ("ldf", ctypes.c_int64), ("ld_gate", ctypes.c_int64), ("eps", ctypes.c_float),
+                ("alpha", ctypes.c_float), ("p", ctypes.c_double), ("site", ctypes.c_int64)]
+
+
+class JoinTensors(ctypes.Structure):        # inputs of a join, and their gradients
+    _fields_ = [(k, ctypes.c_void_p) for k in ("x", "f", "post_weight", "post_bias", "gate", "scale", "pre_weight",
+                                               "pre_bias")]
 
 
 class SlorrError(RuntimeError):
@@ -119,6 +143,17 @@ def lib() -> ctypes.CDLL:
         L.slorr_plan_get_launches.restype = ctypes.c_int
         L.slorr_plan_get_kernels.argtypes = [vp, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double)]
         L.slorr_plan_get_kernels.restype = ctypes.c_int
+        pf, pj, pt, psz = (ctypes.POINTER(t) for t in (Ffn, Join, JoinTensors, sz))
+        L.slorr_ffn_sizes.argtypes = [pf, psz, psz, psz]
+        L.slorr_ffn_forward.argtypes = [pf] + [vp] * 7 + [sz, vp]
+        L.slorr_ffn_backward.argtypes = [pf] + [vp] * 11 + [sz, vp]
+        L.slorr_join_forward.argtypes = [pj, pt, vp, vp, vp, vp]
+        L.slorr_join_workspace.argtypes = [pj, psz]
+        L.slorr_join_backward.argtypes = [pj, pt, vp, vp, vp, pt, vp, sz, vp]
+        L.slorr_dropout.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.c_double, vp, ctypes.c_int64, vp, vp, vp]
+        for f in ("slorr_ffn_sizes", "slorr_ffn_forward", "slorr_ffn_backward", "slorr_join_forward",
+                  "slorr_join_workspace", "slorr_join_backward", "slorr_dropout"):
+            getattr(L, f).restype = ctypes.c_int
         L.slorr_status_string.argtypes = [ctypes.c_int]
         L.slorr_status_string.restype = ctypes.c_char_p
         L.slorr_last_error.argtypes = []

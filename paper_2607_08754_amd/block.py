@@ -1,0 +1,402 @@
+"""Operators of a regularised feed-forward block: argument marshalling and
+autograd plumbing only; every step runs in libslorr.so.
+
+  gated_ffn          y = (act(x Wg^T) * (x Wu^T)) Wd^T
+  block_norm         RMS or layer norm of a block's input
+  block_join         y = x + alpha * scale * gate * dropout(norm(f)) and the next
+                     block's norm of y, in one kernel
+  dropout            dropout from a counter-based generator; no mask is stored
+  FeedForwardBlock   these as a module, whose projections are the weights that
+                     Regularizer and DecoupledSlorr take
+
+Tensors are float32 or bfloat16, all of a call of one dtype, on one GPU; the
+last dimension is the row. Activations may be strided (a layout that the
+kernels do not read in place is copied); weights are contiguous. Calls run on
+the current stream of the tensors' device and can be captured into a graph.
+Gradients are formed for the inputs that require them. Each is written anew by
+fixed-order sums: no atomics, so results repeat bit for bit.
+
+Dropout draws its numbers from rng, an int64 tensor (key, offset) on the device,
+and an integer site that sets the calls of one step apart. The backward pass
+draws them again, so rng keeps its values until then: a training loop advances
+the offset once per step, by more than its largest site.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import List, Optional, Tuple
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import _lib
+from ._lib import check, lib
+
+__all__ = ["gated_ffn", "block_norm", "block_join", "dropout", "FeedForwardBlock"]
+
+_DTYPE = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
+_ACT = {"silu": _lib.SILU, "gelu": _lib.GELU, "gelu_tanh": _lib.GELU_TANH}
+_NORM = {"rms": _lib.RMS, "layer": _lib.LAYER}
+_MAX_STRIDE = (1 << 22) - 8
+
+
+def _check_first(x: torch.Tensor, name: str) -> int:
+    if not isinstance(x, torch.Tensor) or x.dtype not in _DTYPE:
+        raise ValueError(f"{name} must be a float32 or bfloat16 tensor")
+    if x.device.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"{name} must have a last dimension of at least 1")
+    return _DTYPE[x.dtype]
+
+
+def _check_like(t: Optional[torch.Tensor], shape, x: torch.Tensor, name: str) -> None:
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != x.dtype or t.device != x.device:
+        raise ValueError(f"{name} must be a {x.dtype} {tuple(shape)} tensor on {x.device}")
+
+
+def _check_vector(t, shape, x, name):
+    _check_like(t, shape, x, name)
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _rows(t: torch.Tensor, dim: int) -> Tuple[torch.Tensor, int]:
+    """t as rows of dim values, 16-byte aligned, and the stride of its rows."""
+    m = t if t.dim() == 2 else t.reshape(-1, dim)
+    n, ld = m.shape[0], m.stride(0)
+    if (dim > 1 and m.stride(1) != 1) or (n > 1 and not dim <= ld <= _MAX_STRIDE) or m.data_ptr() % 16:
+        m = m.clone(memory_format=torch.contiguous_format)
+        ld = dim
+    return m, ld if n > 1 else dim
+
+
+def _stream(t: torch.Tensor) -> int:
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _bytes(n: int, like: torch.Tensor) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.uint8, device=like.device)
+
+
+# ------------------------------------------------------------- feed-forward
+
+def _ffn_block(x, ldx, w_gate, act, lddy=0):
+    return _lib.Ffn(x.shape[0], w_gate.shape[1], w_gate.shape[0], _DTYPE[x.dtype], act, ldx, lddy)
+
+
+def _ffn_forward(x, ldx, w_gate, w_up, w_down, act, keep):
+    """y (tokens, dim) and, with keep, the state of the backward pass."""
+    with torch.cuda.device(x.device):
+        d = _ffn_block(x, ldx, w_gate, act)
+        st, ws = ctypes.c_size_t(), ctypes.c_size_t()
+        check(lib().slorr_ffn_sizes(d, st, ws, None), "slorr_ffn_sizes")
+        y = torch.empty((x.shape[0], x.shape[1]), dtype=x.dtype, device=x.device)
+        state = _bytes(st.value, x) if keep else None
+        work = _bytes(ws.value, x)
+        check(lib().slorr_ffn_forward(d, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
+                                      y.data_ptr(), _ptr(state), work.data_ptr(), ws.value, _stream(x)),
+              "slorr_ffn_forward")
+    return y, state
+
+
+class _GatedFfn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, act):
+        rows, ldx = _rows(x, x.shape[-1])
+        y, state = _ffn_forward(rows, ldx, w_gate, w_up, w_down, act, True)
+        ctx.act, ctx.ldx, ctx.shape = act, ldx, x.shape
+        ctx.save_for_backward(rows, w_gate, w_up, w_down, state)
+        return y.view(x.shape)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, w_gate, w_up, w_down, state = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        with torch.cuda.device(x.device):
+            dy, lddy = _rows(dy, x.shape[1])
+            d = _ffn_block(x, ctx.ldx, w_gate, ctx.act, lddy)
+            ws = ctypes.c_size_t()
+            check(lib().slorr_ffn_sizes(d, None, None, ws), "slorr_ffn_sizes")
+            grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if n else None
+                     for t, n in zip((x, w_gate, w_up, w_down), need)]
+            work = _bytes(ws.value, x)
+            check(lib().slorr_ffn_backward(d, dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
+                                           w_down.data_ptr(), state.data_ptr(), *map(_ptr, grads), work.data_ptr(),
+                                           ws.value, _stream(x)), "slorr_ffn_backward")
+        if grads[0] is not None:
+            grads[0] = grads[0].view(ctx.shape)
+        return (*grads, None)
+
+
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+              act: str = "silu") -> torch.Tensor:
+    """y = (act(x Wg^T) * (x Wu^T)) Wd^T over the rows of x (..., dim).
+
+    w_gate, w_up: (inner, dim), w_down: (dim, inner), contiguous. act: "silu",
+    "gelu" or "gelu_tanh". In bfloat16 the inner activations are rounded to
+    bfloat16 between the products. Without gradients nothing is kept."""
+    _check_first(x, "x")
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {list(_ACT)}")
+    dim = x.shape[-1]
+    if w_gate.dim() != 2 or w_gate.shape[0] < 1:
+        raise ValueError("w_gate must be a matrix of at least one row")
+    inner = w_gate.shape[0]
+    for t, shape, name in ((w_gate, (inner, dim), "w_gate"), (w_up, (inner, dim), "w_up"), (w_down, (dim, inner), "w_down")):
+        _check_vector(t, shape, x, name)
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down)):
+        return _GatedFfn.apply(x, w_gate, w_up, w_down, _ACT[act])
+    rows, ldx = _rows(x, dim)
+    return _ffn_forward(rows, ldx, w_gate, w_up, w_down, _ACT[act], False)[0].view(x.shape)
+
+
+# --------------------------------------------------------------------- join
+
+_JOIN = ("x", "f", "post_weight", "post_bias", "gate", "scale", "pre_weight", "pre_bias")
+
+
+def _join_run(d, tensors, rng, want_y):
+    """The forward call on laid-out inputs: y and z (None where absent)."""
+    x = tensors[0]
+    with torch.cuda.device(x.device):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
+        z = torch.empty(x.shape, dtype=x.dtype, device=x.device) if d.flags & _lib.JOIN_PRE else None
+        check(lib().slorr_join_forward(d, _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
+                                       _stream(x)), "slorr_join_forward")
+    return y, z
+
+
+class _Join(torch.autograd.Function):
+    """forward(d, shapes, rng, *tensors): tensors are laid out by _join_inputs
+    in the order of _JOIN; d describes the call. Returns (y, z), or z alone
+    without f."""
+
+    @staticmethod
+    def forward(ctx, d, rng, *tensors):
+        laid = _join_layout(d, tensors)
+        y, z = _join_run(d, laid, rng, laid[1] is not None)
+        ctx.d = d
+        ctx.shapes = [None if t is None else t.shape for t in tensors]
+        ctx.save_for_backward(rng, *laid)
+        ctx.set_materialize_grads(False)
+        shape = tensors[0].shape
+        outs = tuple(t.view(shape) for t in (y, z) if t is not None)
+        return outs if len(outs) > 1 else outs[0]
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *douts):
+        rng, *laid = ctx.saved_tensors
+        d, x = ctx.d, laid[0]
+        if all(t is None for t in douts):
+            return (None,) * (2 + len(laid))
+        with torch.cuda.device(x.device):
+            douts = [None if t is None else _dense(t, x.shape[1]) for t in douts]
+            dy = douts[0] if laid[1] is not None else None
+            dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
+            grads = [torch.empty(s, dtype=x.dtype, device=x.device) if n else None
+                     for s, n in zip(ctx.shapes, ctx.needs_input_grad[2:])]
+            ws = ctypes.c_size_t()
+            check(lib().slorr_join_workspace(d, ws), "slorr_join_workspace")
+            work = _bytes(ws.value, x)
+            check(lib().slorr_join_backward(d, _lib.JoinTensors(*map(_ptr, laid)), _ptr(rng), _ptr(dy), _ptr(dz),
+                                            _lib.JoinTensors(*map(_ptr, grads)), work.data_ptr(), ws.value,
+                                            _stream(x)), "slorr_join_backward")
+        return (None, None, *grads)
+
+
+def _dense(t: torch.Tensor, dim: int) -> torch.Tensor:
+    m = t.reshape(-1, dim).contiguous()
+    return m if m.data_ptr() % 16 == 0 else m.clone()
+
+
+def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
+    """The inputs as the library reads them; the row strides go into d."""
+    dim = d.dim
+    out = [None if t is None else t.detach() for t in tensors]
+    out[0], d.ldx = _rows(out[0], dim)
+    if out[1] is not None:
+        out[1], d.ldf = _rows(out[1], dim)
+    if out[4] is not None:
+        out[4], d.ld_gate = _rows(out[4], dim)
+    return out
+
+
+def _gate_rows(gate: torch.Tensor, x: torch.Tensor) -> int:
+    """Rows of a gate over x: (dim,), or x's shape with trailing dimensions
+    before the last set to 1."""
+    if gate.dim() == 1:
+        return 1
+    if gate.dim() == x.dim():
+        lead, rows = True, 1
+        for g, n in zip(gate.shape[:-1], x.shape[:-1]):
+            if lead and g == n:
+                rows *= g
+            elif g == 1:
+                lead = False
+            else:
+                rows = 0
+                break
+        else:
+            return rows
+    raise ValueError("gate must have shape (dim,), or x's shape with its trailing dimensions before the last set to 1")
+
+
+def _check_rng(p: float, rng, x: torch.Tensor) -> None:
+    if not 0.0 <= p < 1.0:
+        raise ValueError("p must be in [0, 1)")
+    if rng is None:
+        if p > 0.0:
+            raise ValueError("dropout needs rng")
+    elif rng.dtype != torch.int64 or rng.shape != (2,) or not rng.is_contiguous() or rng.device != x.device:
+        raise ValueError(f"rng must be an int64 tensor of two values on {x.device}")
+
+
+def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
+    if kind not in _NORM:
+        raise ValueError(f"kind must be one of {list(_NORM)}")
+    dim, gate = x.shape[-1], tensors[4]
+    for t, name in zip(tensors, _JOIN):
+        if name in ("x", "gate"):
+            continue
+        if name == "f":
+            _check_like(t, x.shape, x, name)
+        else:
+            _check_vector(t, (dim,), x, name)
+    rows = x.numel() // dim
+    d = _lib.Join(rows, dim, _DTYPE[x.dtype], _NORM[kind], (_lib.JOIN_POST if post else 0) | (_lib.JOIN_PRE if pre else 0),
+                  0, 0, 0, 0, float(eps), float(alpha), float(p), int(site))
+    if gate is not None:
+        _check_like(gate, (*gate.shape[:-1], dim), x, "gate")
+        d.gate_rows = _gate_rows(gate, x)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        return _Join.apply(d, rng, *tensors)
+    y, z = _join_run(d, _join_layout(d, tensors), rng, f is not None)
+    outs = tuple(t.view(x.shape) for t in (y, z) if t is not None)
+    return outs if len(outs) > 1 else outs[0]
+
+
+def block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               kind: str = "rms", eps: float = 1e-5) -> torch.Tensor:
+    """The norm of a block's input over the last dimension (at most 8192):
+    kind "rms" or "layer", times weight plus bias (each (dim,) or None)."""
+    _check_first(x, "x")
+    return _join_call(x, None, kind, eps, False, True, (x, None, None, None, None, None, weight, bias), 1.0, 0.0, None, 0)
+
+
+def block_join(x: torch.Tensor, f: torch.Tensor, *, post: Optional[bool] = None,
+               post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+               gate: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, alpha: float = 1.0,
+               pre: Optional[bool] = None, pre_weight: Optional[torch.Tensor] = None,
+               pre_bias: Optional[torch.Tensor] = None, kind: str = "rms", eps: float = 1e-5, p: float = 0.0,
+               rng: Optional[torch.Tensor] = None, site: int = 0) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """The join between two blocks: y = x + alpha * scale * gate * dropout(u),
+    u = norm(f) * post_weight + post_bias (u = f with post=False), and
+    z = norm(y) * pre_weight + pre_bias (None with pre=False). Returns (y, z).
+
+    x, f: (..., dim), dim at most 8192. post, pre: whether the norm is there; by
+    default where one of its vectors is given. Vectors and scale: (dim,). gate:
+    (dim,), x's shape, or x's shape with trailing dimensions before the last set
+    to 1 (one gate row per sequence). p, rng, site: residual dropout, as in
+    dropout()."""
+    _check_first(x, "x")
+    if f is None:
+        raise ValueError("f is required (block_norm is the norm alone)")
+    post = (post_weight is not None or post_bias is not None) if post is None else bool(post)
+    pre = (pre_weight is not None or pre_bias is not None) if pre is None else bool(pre)
+    if not post and (post_weight is not None or post_bias is not None):
+        raise ValueError("post_weight or post_bias with post=False")
+    if not pre and (pre_weight is not None or pre_bias is not None):
+        raise ValueError("pre_weight or pre_bias with pre=False")
+    _check_rng(p, rng, x)
+    out = _join_call(x, f, kind, eps, post, pre, (x, f, post_weight, post_bias, gate, scale, pre_weight, pre_bias),
+                     alpha, p, rng, site)
+    return out if pre else (out, None)
+
+
+# ------------------------------------------------------------------ dropout
+
+def _dropout_run(x: torch.Tensor, p: float, rng, site: int) -> torch.Tensor:
+    with torch.cuda.device(x.device):
+        x = x.contiguous()
+        if x.data_ptr() % 16:
+            x = x.clone()
+        y = torch.empty_like(x)
+        check(lib().slorr_dropout(x.numel(), _DTYPE[x.dtype], p, _ptr(rng), site, x.data_ptr(), y.data_ptr(), _stream(x)),
+              "slorr_dropout")
+    return y
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, rng, site):
+        ctx.p, ctx.site = p, site
+        ctx.save_for_backward(rng)
+        return _dropout_run(x, p, rng, site)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return _dropout_run(dy, ctx.p, ctx.saved_tensors[0], ctx.site), None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, rng: Optional[torch.Tensor], site: int = 0) -> torch.Tensor:
+    """x / (1 - p) where an element is kept, else 0. Element e of x (in row-major
+    order) is kept by its 16-bit number of the Philox4x32-10 sequence with key
+    rng[0] and offset rng[1] + site, so p counts in steps of 2^-16 (rounded to
+    the nearest; the factor is that of the rounded p)."""
+    _check_first(x, "x")
+    _check_rng(p, rng, x)
+    if torch.is_grad_enabled() and x.requires_grad:
+        return _Dropout.apply(x, float(p), rng, int(site))
+    return _dropout_run(x, float(p), rng, int(site))
+
+
+# ------------------------------------------------------------------- module
+
+class FeedForwardBlock(torch.nn.Module):
+    """A pre-norm gated feed-forward block with its residual path:
+    forward(x) = x + scale * dropout(norm(ffn(norm(x)))).
+
+    matrices() are the projections, the weights to regularise. post: a norm
+    after the feed-forward; scale: a residual scale per channel, starting at
+    that value (None: none); p: residual dropout in training, from rng and site
+    (see dropout)."""
+
+    def __init__(self, dim: int, inner: int, act: str = "silu", kind: str = "rms", eps: float = 1e-5,
+                 post: bool = False, scale: Optional[float] = None, p: float = 0.0, device=None,
+                 dtype: torch.dtype = torch.bfloat16):
+        super().__init__()
+        kw = dict(device=device, dtype=dtype)
+        self.act, self.kind, self.eps, self.p = act, kind, eps, p
+
+        def matrix(r, c):
+            return torch.nn.Parameter(torch.randn(r, c, **kw) * c ** -0.5)
+
+        def vector(value):
+            return torch.nn.Parameter(torch.full((dim,), float(value), **kw))
+
+        self.w_gate, self.w_up, self.w_down = matrix(inner, dim), matrix(inner, dim), matrix(dim, inner)
+        self.pre_weight = vector(1)
+        self.pre_bias = vector(0) if kind == "layer" else None
+        self.post_weight = vector(1) if post else None
+        self.post_bias = vector(0) if post and kind == "layer" else None
+        self.scale = None if scale is None else vector(scale)
+
+    def matrices(self) -> List[torch.nn.Parameter]:
+        return [self.w_gate, self.w_up, self.w_down]
+
+    def forward(self, x: torch.Tensor, rng: Optional[torch.Tensor] = None, site: int = 0) -> torch.Tensor:
+        z = block_norm(x, self.pre_weight, self.pre_bias, kind=self.kind, eps=self.eps)
+        f = gated_ffn(z, self.w_gate, self.w_up, self.w_down, act=self.act)
+        p = self.p if self.training else 0.0
+        return block_join(x, f, post_weight=self.post_weight, post_bias=self.post_bias, scale=self.scale, kind=self.kind,
+                          eps=self.eps, p=p, rng=rng if p > 0.0 else None, site=site)[0]

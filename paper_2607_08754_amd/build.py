@@ -23,7 +23,9 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libslorr.so")
 PROBE = os.path.join(PKG, "probe_ceiling")
 
-SOURCES = ["kernels.hip", "api.cpp", "plan.cpp", "pe_schedule.cpp"]
+# the kernels; their objects are joined into one, _build/kernels.o
+DEVICE_SOURCES = ["kernels.hip", "ffn.hip", "join.hip"]
+HOST_SOURCES = ["api.cpp", "plan.cpp", "pe_schedule.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -36,7 +38,8 @@ COMMON = [
 
 
 def _compile(src: str) -> str:
-    obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
+    stem, ext = os.path.splitext(src)
+    obj = os.path.join(BUILD, stem + (".dev.o" if ext == ".hip" else ".o"))
     cmd = [HIPCC, *COMMON, "-c", os.path.join(CSRC, src), "-o", obj]
     if src.endswith(".hip"):
         cmd.append("-Rpass-analysis=kernel-resource-usage")
@@ -61,8 +64,14 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(4, len(SOURCES))) as ex:
-        objs = list(ex.map(_compile, SOURCES))
+    with ThreadPoolExecutor(max_workers=6) as ex:
+        objs = list(ex.map(_compile, DEVICE_SOURCES + HOST_SOURCES))
+    device, objs = objs[:len(DEVICE_SOURCES)], objs[len(DEVICE_SOURCES):]
+    kernels = os.path.join(BUILD, "kernels.o")
+    res = subprocess.run(["ld", "-r", *device, "-o", kernels], capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"joining the kernels' objects failed:\n{res.stdout}\n{res.stderr}")
+    objs.append(kernels)
     tmp = LIB + ".tmp"
     cmd = [HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs,
            f"-Wl,--version-script={os.path.join(CSRC, 'exports.map')}", "-o", tmp]

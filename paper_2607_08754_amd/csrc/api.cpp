@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <list>
 #include <mutex>
@@ -12,6 +13,7 @@
 #include <utility>
 #include <vector>
 
+#include "block.hpp"
 #include "kernels.hpp"
 #include "plan.hpp"
 #include "slorr.h"
@@ -701,3 +703,5 @@ const char *slorr_status_string(slorr_status_t status) {
 const char *slorr_last_error(void) { return g_last_error.c_str(); }
 
 }  // extern "C"
+
+#include "block_api.hpp"

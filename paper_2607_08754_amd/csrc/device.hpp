@@ -1,0 +1,159 @@
+// Device helpers that the library's kernels share: types and conversions, 16-byte
+// accesses, LDS layouts, direct global -> LDS fetches and their waits.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace slorr {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef uint16_t bf16_t;
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(bf16_t v) { return __uint_as_float(uint32_t(v) << 16); }
+__device__ __forceinline__ float to_f(_Float16 v) { return float(v); }
+
+// fp32 -> bf16 with round to nearest, ties to even (a NaN stays a quiet NaN):
+// add half an ulp of the bf16 result, minus one when the kept part is even,
+// then truncate.
+__device__ __forceinline__ bf16_t f32_to_bf16(float x) {
+  uint32_t u = __float_as_uint(x);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return bf16_t((u >> 16) | 0x40u);
+  u += 0x7fffu + ((u >> 16) & 1u);
+  return bf16_t(u >> 16);
+}
+
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ _Float16 from_f<_Float16>(float v) { return _Float16(v); }
+template <> __device__ __forceinline__ bf16_t from_f<bf16_t>(float v) { return f32_to_bf16(v); }
+
+// The full-tile path of the tile kernels below: 16-byte accesses known to be
+// aligned and in bounds, issued as global-memory instructions with no branch
+// between them, so that all of a thread's loads are in flight together (the
+// weight and gradient pointers come from a device table: left to itself the
+// compiler cannot tell their address space and emits flat accesses).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 gload16(const void *p) {
+  return *(const __attribute__((address_space(1))) u32x4 *)p;
+}
+__device__ __forceinline__ void gstore16(void *p, u32x4 v) { *(__attribute__((address_space(1))) u32x4 *)p = v; }
+__device__ __forceinline__ u32x4 gload16_stream(const void *p) {
+  return __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4 *)p);
+}
+
+// Byte offset of 16-byte chunk `chunk` of LDS row `row`. The XOR key
+// (row & 7) ^ ((row >> 3) & 1) permutes the chunks so that (a) any 8
+// consecutive rows (one 8-lane phase of a 16-byte read with 32 banks) use 8
+// distinct chunk positions, and (b) any 16 consecutive rows (a 16-lane phase
+// with 64 banks, where rows of equal parity share a 128-byte bank half) use 8
+// distinct positions per parity.
+__device__ __forceinline__ int swz_key(int row) { return (row & 7) ^ ((row >> 3) & 1); }
+__device__ __forceinline__ int swz(int row, int chunk) { return row * 128 + ((chunk ^ swz_key(row)) << 4); }
+
+// 16 bytes per lane from a buffer straight into LDS: byte voff + soff of the
+// buffer (voff per lane, soff wave-uniform) lands at lds_base + 16 l
+// (lds_base wave-uniform, passed in m0). On the update tile's k loop this
+// form issues at a markedly lower cost than global_load_lds_dwordx4 with a
+// 64-bit address per lane; a load past the buffer's size returns zeros
+// instead of faulting. Device pass only: the host pass of the single-source
+// build just needs the kernel's stub.
+//
+// Issued through inline assembly: the compiler then does not track these LDS
+// writes and puts no wait for them before later LDS reads (it cannot tell
+// that those read the other stage). Completion is the caller's job: each
+// k-slab is waited for by count (s_waitcnt vmcnt) before the block barrier
+// that publishes it.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 buffer_rsrc(const void *base, uint32_t bytes) {
+  const uint64_t b = uint64_t(uintptr_t(base));
+  i32x4 r;
+  r[0] = __builtin_amdgcn_readfirstlane(int(uint32_t(b)));
+  r[1] = __builtin_amdgcn_readfirstlane(int(uint32_t(b >> 32) & 0xffffu));   // stride 0
+  r[2] = __builtin_amdgcn_readfirstlane(int(bytes));                        // size in bytes
+  r[3] = 0x00020000;                                                         // raw 32-bit dwords
+  return r;
+}
+__device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds_base) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t m = __builtin_amdgcn_readfirstlane(lds_base);
+  const uint32_t so = __builtin_amdgcn_readfirstlane(soff);
+  asm volatile("buffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(m), "v"(voff), "s"(rsrc), "s"(so) : "memory");
+#else
+  (void)rsrc;
+  (void)voff;
+  (void)soff;
+  (void)lds_base;
+#endif
+}
+__device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uint32_t soff, void *lds_base) {
+  buffer_load_lds16(rsrc, voff, soff, uint32_t(uintptr_t(lds_base)));
+}
+
+// Transposing LDS read of 16-bit values (ds_read_b64_tr_b16). Within each
+// group of 16 lanes, lane s gives the address of 4 consecutive values: row
+// s / 4, columns 4 (s % 4) .. 4 (s % 4) + 3 of a 4 x 16 block; lane j then
+// holds column j of the block, element i from row i.
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ half4 lds_read_tr16(const void *lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef __attribute__((__vector_size__(4 * sizeof(__fp16)))) __fp16 fp16x4;
+  typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
+  const fp16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4 *)(lds));
+  return __builtin_bit_cast(half4, v);
+#else
+  (void)lds;
+  return half4{};
+#endif
+}
+
+// Byte offset of 16-byte chunk `chunk` of k-row `row`
+// of a [k][n] operand stage (rows of `pitch` bytes). The key 4 (row & 3)
+// spreads the 4 rows x 4 chunks that one half-wave reads with a transposing
+// read (rows r..r+3 of a 16-row step, 64 bytes each) over all 64 banks.
+__device__ __forceinline__ int kn_off(int row, int chunk, int pitch) {
+  return row * pitch + ((chunk ^ ((row & 3) << 2)) << 4);
+}
+
+// LDS byte offset of a shared array. The fetches below take offsets, not
+// pointers: a generic pointer would be cast back to LDS with a null check.
+__device__ __forceinline__ uint32_t lds_offset(const char *smem) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return uint32_t(uintptr_t((const __attribute__((address_space(3))) char *)smem));
+#else
+  (void)smem;
+  return 0;
+#endif
+}
+
+// s_waitcnt vmcnt(N), the other counters left alone (gfx9 encoding).
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// Wait until at most `ahead` (<= A) slabs of fetches, L instructions each,
+// issued by this wave are outstanding.
+template <int L, int A>
+__device__ __forceinline__ void vm_wait_slabs(int ahead) {
+  if constexpr (A >= 2) {
+    if (ahead >= 2) {
+      vm_wait<2 * L>();
+      return;
+    }
+  }
+  if constexpr (A >= 1) {
+    if (ahead >= 1) {
+      vm_wait<L>();
+      return;
+    }
+  }
+  vm_wait<0>();
+}
+
+}  // namespace slorr

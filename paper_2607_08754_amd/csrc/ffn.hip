@@ -1,0 +1,244 @@
+// Gated feed-forward block (see ffn_gemm.hpp for the products):
+//
+//   k_ffn       the products, with the activation and its backward fused into
+//               their epilogues
+//   k_planes    operands laid out in 16-byte rows: bf16 rows padded to a
+//               multiple of 8, fp32 values as three bf16 planes
+//   k_split_sum a product's partials added in order
+#include <algorithm>
+#include <type_traits>
+
+#include "block.hpp"
+#include "ffn_gemm.hpp"
+#include "layout.hpp"
+
+namespace slorr {
+namespace {
+
+void check(hipError_t e, const char *what) {
+  if (e != hipSuccess) throw HipError(std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// rows x cols values -> bf16 rows of ld numbers, zero padded (F32: three planes).
+template <bool F32>
+__global__ __launch_bounds__(256) void k_planes(const void *src, int64_t rows, int32_t cols, int64_t lds, char *dst,
+                                                int32_t ld, int64_t plane) {
+  using T = typename std::conditional<F32, float, uint16_t>::type;
+  const int pieces = ld >> 3;
+  const int64_t total = rows * pieces;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+    const int64_t r = i / pieces;
+    const int c = int(i - r * pieces) * 8;
+    const T *p = static_cast<const T *>(src) + r * lds + c;
+    float v[8];
+    if (c + 8 <= cols && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+      load_whole<F32>(p, 0, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_f(p[j]) : 0.0f;
+    }
+    store_planes<F32>(dst + (r * ld + c) * 2, plane, v);
+  }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_split_sum(FfnProb p) {
+  const int pieces = int(p.ldp >> 3);
+  const int64_t total = int64_t(p.m) * pieces, step = int64_t(p.m) * p.ldp;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+    const int64_t r = i / pieces;
+    const int c = int(i - r * pieces) * 8;
+    float v[8] = {};
+    for (int s = 0; s < p.splits; ++s) {
+      float w[8];
+      load_whole<true>(p.part + s * step, r * p.ldp + c, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += w[j];
+    }
+    if (c < p.n) store_some<F32>(p.out, r * p.ldo + c, p.n - c, v);
+  }
+}
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+template <bool AK, bool BK, int EPI, bool F32>
+void launch_products(FfnArgs &a, hipStream_t st) {
+  constexpr int B = kTile;
+  int64_t units = 0;
+  for (int i = 0; i < a.nprob; ++i) {
+    FfnProb &p = a.p[i];
+    p.tm = int32_t(cdiv(p.m, B));
+    p.tn = int32_t(cdiv(EPI == kStore ? p.n : a.ldf, EPI == kAct ? B / 2 : B));
+    p.splits = 1;
+    p.per = int32_t(cdiv(p.k, 64)) * p.nsrc * (F32 ? 6 : 1);
+    p.unit0 = int32_t(units);
+    units += int64_t(p.tm) * p.tn * p.splits;
+  }
+  a.units = int32_t(units);
+  if (!units) return;
+  hipLaunchKernelGGL((k_ffn<B, B, 2, 2, 2, AK, BK, EPI, F32>), dim3(uint32_t(units)), dim3(256), 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+}
+
+// The state's parts: a, b, and in bf16 a byte per 8 values of each.
+void state_parts(const FfnShape &s, void *state, FfnArgs &a) {
+  if (!state) return;
+  const int64_t n = s.tokens * s.ldf();
+  char *p = static_cast<char *>(state);
+  a.sa = p;
+  a.sb = p + n * s.elem();
+  a.ea = reinterpret_cast<uint8_t *>(p) + 2 * n * s.elem();
+  a.eb = a.ea + n / 8;
+}
+
+// An operand as the products read it.
+struct Operand {
+  const char *p;
+  int64_t ld, plane;
+};
+
+template <bool F32>
+Operand operand(const FfnShape &s, const void *src, int64_t rows, int32_t cols, int64_t lds, char *ws, size_t off,
+                hipStream_t st) {
+  if (off == kAbsent) return {static_cast<const char *>(src), lds, 0};
+  Operand o{ws + off, up8(cols), rows * up8(cols) * 2};
+  const int64_t n = rows * (o.ld / 8);
+  if (n) {
+    const uint32_t grid = uint32_t(std::min<int64_t>(cdiv(n, 256), 8 * kCus));
+    hipLaunchKernelGGL(k_planes<F32>, dim3(grid), dim3(256), 0, st, src, rows, cols, lds, ws + off, int32_t(o.ld), o.plane);
+    check(hipGetLastError(), "kernel launch");
+  }
+  return o;
+}
+
+FfnProb product(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, void *out, int64_t ldo) {
+  FfnProb p{};
+  p.a[0] = a.p;
+  p.b[0] = b.p;
+  p.pa = a.plane;
+  p.pb = b.plane;
+  p.lda = a.ld;
+  p.ldb = b.ld;
+  p.m = int32_t(m);
+  p.n = int32_t(n);
+  p.k = int32_t(k);
+  p.nsrc = 1;
+  p.out = out;
+  p.ldo = ldo;
+  return p;
+}
+
+template <bool F32>
+void forward(const FfnShape &s, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *state,
+             char *ws, hipStream_t st) {
+  const FfnLayout l = ffn_layout(s, false);
+  const int64_t T = s.tokens;
+  const Operand X = operand<F32>(s, x, T, s.dim, s.ldx, ws, l.x, st);
+  const Operand G = operand<F32>(s, wg, s.inner, s.dim, s.dim, ws, l.wg, st);
+  const Operand U = operand<F32>(s, wu, s.inner, s.dim, s.dim, ws, l.wu, st);
+  const Operand D = operand<F32>(s, wd, s.dim, s.inner, s.inner, ws, l.wd, st);
+  const Operand H{ws + l.h, s.ldf(), T * s.ldf() * 2};
+  FfnArgs a{};
+  a.nprob = 1;
+  a.act = s.act;
+  a.ldf = int32_t(s.ldf());
+  a.p[0] = product(X, G, T, s.inner, s.dim, nullptr, 0);
+  a.p[0].b[1] = U.p;
+  state_parts(s, state, a);
+  a.h = ws + l.h;
+  a.plane = H.plane;
+  launch_products<false, false, kAct, F32>(a, st);
+  a.p[0] = product(H, D, T, s.dim, s.inner, y, s.dim);
+  launch_products<false, false, kStore, F32>(a, st);
+}
+
+template <bool F32>
+void backward(const FfnShape &s, const void *dy, const void *x, const void *wg, const void *wu, const void *wd,
+              const void *state, void *dx, void *dwg, void *dwu, void *dwd, char *ws, hipStream_t st) {
+  const FfnLayout l = ffn_layout(s, true);
+  const int64_t T = s.tokens;
+  const Operand DY = operand<F32>(s, dy, T, s.dim, s.lddy, ws, l.dy, st);
+  const int64_t plane = T * s.ldf() * 2;
+  const Operand H{ws + l.h, s.ldf(), plane}, DA{ws + l.da, s.ldf(), plane}, DB{ws + l.db, s.ldf(), plane};
+  FfnArgs a{};
+  a.act = s.act;
+  a.ldf = int32_t(s.ldf());
+  if (T) {
+    const Operand D = operand<F32>(s, wd, s.dim, s.inner, s.inner, ws, l.wd, st);
+    a.nprob = 1;
+    a.p[0] = product(DY, D, T, s.inner, s.dim, nullptr, 0);
+    state_parts(s, const_cast<void *>(state), a);
+    a.h = ws + l.h;
+    a.da = ws + l.da;
+    a.db = ws + l.db;
+    a.plane = plane;
+    launch_products<false, true, kActBack, F32>(a, st);
+  }
+  if (dx && T) {
+    const Operand G = operand<F32>(s, wg, s.inner, s.dim, s.dim, ws, l.wg, st);
+    const Operand U = operand<F32>(s, wu, s.inner, s.dim, s.dim, ws, l.wu, st);
+    a.nprob = 1;
+    a.p[0] = product(DA, G, T, s.dim, s.inner, dx, s.dim);
+    a.p[0].a[1] = DB.p;
+    a.p[0].b[1] = U.p;
+    a.p[0].nsrc = 2;
+    launch_products<false, true, kStore, F32>(a, st);
+  }
+  if (dwg || dwu || dwd) {
+    Operand X{};
+    if (dwg || dwu) X = operand<F32>(s, x, T, s.dim, s.ldx, ws, l.x, st);
+    a.nprob = 0;
+    if (dwg) a.p[a.nprob++] = product(DA, X, s.inner, s.dim, T, dwg, s.dim);
+    if (dwu) a.p[a.nprob++] = product(DB, X, s.inner, s.dim, T, dwu, s.dim);
+    if (dwd) a.p[a.nprob++] = product(DY, H, s.dim, s.inner, T, dwd, s.inner);
+    launch_products<true, true, kStore, F32>(a, st);
+  }
+}
+
+}  // namespace
+
+FfnLayout ffn_layout(const FfnShape &s, bool bwd) {
+  FfnLayout l;
+  const size_t pl = size_t(s.planes()) * 2;
+  auto take = [&](size_t bytes) {
+    const size_t at = l.bytes;
+    l.bytes += (bytes + 255) & ~size_t(255);
+    return at;
+  };
+  const size_t T = size_t(s.tokens), w = size_t(s.inner) * size_t(s.ldd()) * pl;
+  if (!s.direct(s.dim, s.ldx)) l.x = take(T * size_t(s.ldd()) * pl);
+  if (bwd && !s.direct(s.dim, s.lddy)) l.dy = take(T * size_t(s.ldd()) * pl);
+  if (!s.direct(s.dim, s.dim)) {
+    l.wg = take(w);
+    l.wu = take(w);
+  }
+  if (!s.direct(s.inner, s.inner)) l.wd = take(size_t(s.dim) * size_t(s.ldf()) * pl);
+  l.h = take(T * size_t(s.ldf()) * pl);
+  if (bwd) {
+    l.da = take(T * size_t(s.ldf()) * pl);
+    l.db = take(T * size_t(s.ldf()) * pl);
+  }
+  l.bytes = std::max(l.bytes, size_t(256));
+  return l;
+}
+
+size_t ffn_state_bytes(const FfnShape &s) {
+  const size_t n = size_t(s.tokens) * size_t(s.ldf());
+  return std::max(size_t(256), 2 * n * s.elem() + (s.dtype == SLORR_BF16 ? n / 4 : 0));
+}
+
+void enqueue_ffn_forward(const FfnShape &s, const void *x, const void *wg, const void *wu, const void *wd, void *y,
+                         void *state, void *ws, hipStream_t st) {
+  if (!s.tokens) return;
+  if (s.dtype == SLORR_F32) forward<true>(s, x, wg, wu, wd, y, state, static_cast<char *>(ws), st);
+  else forward<false>(s, x, wg, wu, wd, y, state, static_cast<char *>(ws), st);
+}
+
+void enqueue_ffn_backward(const FfnShape &s, const void *dy, const void *x, const void *wg, const void *wu,
+                          const void *wd, const void *state, void *dx, void *dwg, void *dwu, void *dwd, void *ws,
+                          hipStream_t st) {
+  if (s.dtype == SLORR_F32) backward<true>(s, dy, x, wg, wu, wd, state, dx, dwg, dwu, dwd, static_cast<char *>(ws), st);
+  else backward<false>(s, dy, x, wg, wu, wd, state, dx, dwg, dwu, dwd, static_cast<char *>(ws), st);
+}
+
+}  // namespace slorr

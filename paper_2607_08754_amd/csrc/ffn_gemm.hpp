@@ -1,0 +1,485 @@
+// The products of the gated feed-forward block on bf16 MFMA (device code).
+//
+//   forward   a = x Wg^T, b = x Wu^T, h = act(a) b     one kernel, both products
+//             y = h Wd^T
+//   backward  dh = dy Wd, then da = dh b act'(a), db = dh act(a) and h again
+//             in the same kernel;
+//             dx = da Wg + db Wu (one sum over both)
+//             dWg = da^T x, dWu = db^T x, dWd = dy^T h (one launch)
+//
+// Every product is C = A B^T with A, B given either by rows (k contiguous) or
+// as [k][row] (transposed while it is read from LDS), so no operand is
+// transposed in memory.
+//
+// fp32 operands are held as three bf16 numbers (planes) hi + mid + lo, which
+// carry all 24 significand bits over fp32's whole range; a product is the sum
+// of the six plane products whose terms reach 2^-24 of it, the small ones
+// first: lo hi, mid mid, hi lo, mid hi, hi mid, hi hi. The kernels run them as six passes
+// over k into one accumulator. fp32 MFMA has 1/16 of the bf16 rate: six bf16
+// products cost 6/16 of one fp32 product. An infinity gives NaN (infinity times
+// a zero plane).
+#pragma once
+#include "device.hpp"
+
+namespace slorr {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+
+enum FfnEpi { kStore = 0, kAct = 1, kActBack = 2 };
+
+struct FfnProb {               // one product C (m x n) = sum over sources of A B^T
+  const char *a[2], *b[2];     // sources; kAct: b[0], b[1] are both products' rows, one source
+  int64_t pa, pb;              // bytes from one plane to the next
+  int64_t lda, ldb;            // elements per row
+  int32_t m, n, k, nsrc;
+  int32_t tm, tn;              // tiles
+  int32_t splits, per;         // parts of the k range, slabs per part
+  int32_t unit0;               // the first block of this product in the launch
+  void *out;
+  int64_t ldo;
+  float *part;                 // splits > 1: fp32 partials [split][m][ldp]
+  int64_t ldp;
+};
+
+struct FfnArgs {
+  FfnProb p[3];
+  int32_t nprob, units, act;
+  int32_t ldf;                 // row length of the inner tensors
+  void *sa, *sb;               // a, b as kept for the backward pass (kAct: may be null)
+  uint8_t *ea, *eb;            // their exponents (bf16 tensors)
+  char *h, *da, *db;           // bf16 planes
+  int64_t plane;               // bytes from one plane of h, da, db to the next
+};
+
+// act(a) and its derivative. fp32 results take the accurate exponential and
+// division; for bf16 results the hardware's (errors near 2^-20) are far below
+// the rounding that follows.
+template <bool F32>
+__device__ __forceinline__ float sigmoid(float a) {
+  if constexpr (F32) return 1.0f / (1.0f + expf(-a));
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-a));
+}
+template <bool F32>
+__device__ __forceinline__ void act_and_slope(int act, float a, float &f, float &s) {
+  if (act == SLORR_SILU) {
+    const float g = sigmoid<F32>(a);
+    f = a * g;
+    s = g * (1.0f + a * (1.0f - g));
+  } else if (act == SLORR_GELU) {
+    const float c = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+    f = a * c;
+    s = c + a * (F32 ? expf(-0.5f * a * a) : __expf(-0.5f * a * a)) * 0.39894228040143268f;
+  } else {                     // 0.5 a (1 + tanh u) = a sigmoid(2 u)
+    const float k = 1.5957691216057308f, q = 0.044715f * a * a;
+    const float g = sigmoid<F32>(k * a * (1.0f + q));
+    f = a * g;
+    s = g + f * (1.0f - g) * k * (1.0f + 3.0f * q);
+  }
+}
+
+// The three planes of fp32 values: each is the nearest bf16 number to what the
+// ones before it leave (the largest finite one where that would be infinity).
+__device__ __forceinline__ uint16_t bf16_near(float v) {
+  const uint32_t u = __float_as_uint(v);
+  if ((u & 0x7f800000u) == 0x7f800000u) return f32_to_bf16(v);
+  uint16_t r = f32_to_bf16(v);
+  return (r & 0x7fffu) == 0x7f80u ? uint16_t(r - 1) : r;
+}
+__device__ __forceinline__ void planes_of(float v, uint16_t (&p)[3]) {
+  p[0] = bf16_near(v);
+  float r = v - to_f(p[0]);
+  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) r = 0.0f;
+  p[1] = f32_to_bf16(r);
+  p[2] = f32_to_bf16(r - to_f(p[1]));
+}
+
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+
+// 8 values as bf16 (one rounding) or as three planes `plane` bytes apart.
+template <bool F32>
+__device__ __forceinline__ void store_planes(char *p, int64_t plane, const float (&v)[8]) {
+  if constexpr (!F32) {
+    floatx8 f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = v[j];
+    *reinterpret_cast<bf16x8 *>(p) = __builtin_convertvector(f, bf16x8);
+  } else {
+    u16x8 q[3];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint16_t t[3];
+      planes_of(v[j], t);
+#pragma unroll
+      for (int c = 0; c < 3; ++c) q[c][j] = t[c];
+    }
+#pragma unroll
+    for (int c = 0; c < 3; ++c) *reinterpret_cast<u16x8 *>(p + c * plane) = q[c];
+  }
+}
+
+// 8 values of the tensors' type, 16-byte aligned and whole.
+template <bool F32>
+__device__ __forceinline__ void store_whole(void *base, int64_t at, const float (&v)[8]) {
+  if constexpr (!F32) {
+    store_planes<false>(static_cast<char *>(base) + at * 2, 0, v);
+  } else {
+    float4v *p = reinterpret_cast<float4v *>(static_cast<float *>(base) + at);
+    p[0] = float4v{v[0], v[1], v[2], v[3]};
+    p[1] = float4v{v[4], v[5], v[6], v[7]};
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void load_whole(const void *base, int64_t at, float (&v)[8]) {
+  if constexpr (!F32) {
+    const bf16x8 h = *reinterpret_cast<const bf16x8 *>(static_cast<const char *>(base) + at * 2);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = float(h[j]);
+  } else {
+    const float4v *p = reinterpret_cast<const float4v *>(static_cast<const float *>(base) + at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = p[j >> 2][j & 3];
+  }
+}
+// a and b as kept for the backward pass. fp32 tensors: as they are. bf16 tensors:
+// 16-bit integers with one power of two per 8 values, a step of 2^-15 of the
+// largest of the eight at most. bf16 would be as long, but the gradients of a
+// and b would carry its rounding twice more (the gradients of a block of 16384
+// x 1536 x 6144 are off by 3.5e-3 of their size with it; one rounding of the
+// exact ones is 1.7e-3). Eight values with an infinity or a NaN among them are
+// kept in bf16, marked by the exponent 255.
+template <bool F32>
+__device__ __forceinline__ void store_kept(void *base, uint8_t *exps, int64_t at, const float (&v)[8]) {
+  if constexpr (F32) {
+    store_whole<true>(base, at, v);
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+    const int e = max(int(m >> 23), 1);
+    u16x8 q;
+    if (e == 255) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = f32_to_bf16(v[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = uint16_t(int16_t(min(rintf(ldexpf(v[j], 141 - e)), 32767.0f)));
+    }
+    *reinterpret_cast<u16x8 *>(static_cast<uint16_t *>(base) + at) = q;
+    exps[at >> 3] = uint8_t(e);
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void load_kept(const void *base, const uint8_t *exps, int64_t at, float (&v)[8]) {
+  if constexpr (F32) {
+    load_whole<true>(base, at, v);
+  } else {
+    const u16x8 q = *reinterpret_cast<const u16x8 *>(static_cast<const uint16_t *>(base) + at);
+    const int e = exps[at >> 3];
+    if (e == 255) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = to_f(bf16_t(q[j]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = ldexpf(float(int16_t(q[j])), e - 141);
+    }
+  }
+}
+// the first n of 8 values (8: whole when the address allows it)
+template <bool F32>
+__device__ __forceinline__ void store_some(void *base, int64_t at, int n, const float (&v)[8]) {
+  using T = typename std::conditional<F32, float, uint16_t>::type;
+  T *p = static_cast<T *>(base) + at;
+  if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    store_whole<F32>(base, at, v);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < n) p[j] = from_f<T>(v[j]);
+}
+
+// ---------------------------------------------------------------------------
+// Block tile BM x BN, wave tiles of FM x FN MFMA tiles of 32 x 32, slabs of 64
+// k in NS LDS stages: slab i + NS - 1 is fetched while slab i is multiplied;
+// each is waited for by count, then one block barrier publishes it and frees
+// the stage of the slab before it.
+//
+// LDS stages: an operand given by rows is 128-byte rows of 64 k (swz); one
+// given as [k][row] is 64 k-rows of 2 BM (2 BN) bytes (kn_off), read with the
+// transposing LDS load. Fetches go through buffer resources whose size ends at
+// the operand's last valid byte from the slab's corner on: rows past the end
+// read as zeros, as do [k][row] k past the end; chunks past the end of a
+// row's k are sent outside the resource by their offset.
+//
+// kAct: each wave's 64 columns are 32 columns of a and the same 32 of b, by
+// the order in which the rows of Wg and Wu are placed in the stage.
+template <int BM_, int BN_, int WGM_, int WGN_, int NS_, bool AK, bool BK>
+struct FfnTile {
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, NS = NS_;
+  static constexpr int kWaves = WGM * WGN, kThreads = 64 * kWaves;
+  static constexpr int WTM = BM / WGM, WTN = BN / WGN, FM = WTM / 32, FN = WTN / 32;
+  static constexpr int kStageA = BM * 128, kStage = kStageA + BN * 128;
+  static constexpr int kFW = 4;                        // waves that fetch (one per SIMD)
+  static constexpr int kLoadsA = BM / 8 / kFW, kLoadsB = BN / 8 / kFW;
+  static constexpr int kPitch = WTN + 4;               // floats per staged row of the epilogue
+  static constexpr int kEpi = kWaves * 32 * kPitch * 4;
+  static constexpr int kSmem = NS * kStage > kEpi ? NS * kStage : kEpi;
+  static_assert(WTN == 64 && WTM % 32 == 0, "wave tile");
+  static_assert(kWaves >= kFW && BM % 64 == 0 && BN % 64 == 0, "fetches");
+  static_assert(kSmem <= 160 * 1024 && (NS - 2) * (kLoadsA + kLoadsB) < 64, "LDS, vmcnt range");
+  static_assert((!AK || BM >= 128) && (!BK || BN >= 128), "kn_off's key needs 16 chunks per k-row");
+};
+
+// An operand fragment of 32 rows for k step s of a slab: lane l holds 8
+// consecutive k, from 16 s + 8 (l / 32) on, of row l % 32.
+template <bool KM, int PITCH>
+__device__ __forceinline__ bf16x8 ffn_frag(const char *st, int row0, int s, int lane) {
+  if constexpr (KM) {
+    const int g = lane >> 4, si = lane & 15;
+    const int row = 16 * s + 8 * (g >> 1) + (si >> 2);
+    const int col = row0 + 16 * (g & 1) + 4 * (si & 3);
+    const int off = kn_off(row, col >> 3, PITCH) + 8 * (si & 1);
+    const half4 lo = lds_read_tr16(st + off);
+    const half4 hi = lds_read_tr16(st + off + 4 * PITCH);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    return *reinterpret_cast<const bf16x8 *>(st + swz(row0 + (lane & 31), 2 * s + (lane >> 5)));
+  }
+}
+
+// The planes of pass i of an fp32 product, small terms first: A's plane in the
+// low two bits, B's above.
+__device__ __forceinline__ int plane_pair(int i) {
+  // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+  constexpr uint32_t t = 2u | (5u << 4) | (8u << 8) | (1u << 12) | (4u << 16) | (0u << 20);
+  return int((t >> (4 * i)) & 15u);
+}
+
+template <int BM, int BN, int WGM, int WGN, int NS, bool AK, bool BK, int EPI, bool F32>
+__global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
+  using S = FfnTile<BM, BN, WGM, WGN, NS, AK, BK>;
+  constexpr int FM = S::FM, FN = S::FN, FW = S::kFW;
+  __shared__ __attribute__((aligned(16))) char smem[S::kSmem];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lr = lane & 31, lk = lane >> 5;
+  const int wm = wave / WGN, wn = wave % WGN;
+
+  // Block -> unit: each XCD (block index modulo 8) takes a run of consecutive
+  // units, in which 8 tiles of one column of tiles follow each other, so the
+  // blocks of an XCD share operand panels in its L2.
+  int unit;
+  {
+    const int b = int(blockIdx.x), xcd = b & 7, per = args.units >> 3, rem = args.units & 7;
+    unit = xcd * per + min(xcd, rem) + (b >> 3);
+  }
+  FfnProb pr = args.p[0];
+  if (args.nprob > 1 && unit >= args.p[1].unit0) pr = args.p[1];
+  if (args.nprob > 2 && unit >= args.p[2].unit0) pr = args.p[2];
+  unit -= pr.unit0;
+  const int tiles = pr.tm * pr.tn;
+  const int split = unit / tiles;
+  int m0, n0;
+  {
+    const int t = unit - split * tiles, gsize = 8 * pr.tn, g = t / gsize, r = t - g * gsize;
+    const int rows = min(8, pr.tm - 8 * g), c = r / rows;
+    m0 = (8 * g + r - c * rows) * BM;
+    n0 = c * (EPI == kAct ? BN / 2 : BN);
+  }
+  // k: nsrc (times six passes) segments of nkt slabs; this block's slabs [s0, s1)
+  const int nkt = (pr.k + 63) >> 6;
+  const int kp = (pr.k + 7) & ~7;
+  const int nseg = (F32 ? 6 : 1) * pr.nsrc;
+  const int s0 = split * pr.per, s1 = min(nseg * nkt, s0 + pr.per), ns = s1 - s0;
+  int seg = nkt ? s0 / nkt : 0, kt = s0 - seg * nkt;      // the next slab to fetch
+
+  const uint32_t lds0 = lds_offset(smem);
+  auto clamp31 = [](int64_t v) { return uint32_t(v < 0x7fffffff ? v : 0x7fffffff); };
+  // rows: `limit` valid rows from the tile's first on
+  auto fetch_rows = [&](const char *base, int64_t ld, int64_t limit, int k0, uint32_t dst, int i, int row_step) {
+    const i32x4 rs = buffer_rsrc(base + int64_t(k0) * 2, limit > 0 ? clamp31(((limit - 1) * ld + kp - k0) * 2) : 0u);
+    const int row = wave * 8 + (lane >> 3), c = (lane & 7) ^ swz_key(row);
+    uint32_t voff = (uint32_t(row) * uint32_t(ld) + uint32_t(c * 8)) * 2u;
+    if (k0 + 64 > kp && k0 + c * 8 >= kp) voff = 0x80000000u;
+    buffer_load_lds16(rs, voff, uint32_t(row_step) * uint32_t(ld) * 2u, dst + (wave + i * FW) * 1024);
+  };
+  auto fetch_kn = [&](const char *base, int64_t ld, int pitch, int k0, int cols, uint32_t dst, int loads) {
+    const i32x4 rs = buffer_rsrc(base + int64_t(k0) * ld * 2, clamp31((int64_t(pr.k - k0 - 1) * ld + cols) * 2));
+    const int cpr = pitch / 16, rpx = 1024 / pitch;
+    const int row = wave * rpx + lane / cpr;
+    const uint32_t voff = (uint32_t(row) * uint32_t(ld) + uint32_t(((lane % cpr) ^ ((row & 3) << 2)) * 8)) * 2u;
+    for (int i = 0; i < loads; ++i)
+      buffer_load_lds16(rs, voff, uint32_t(i * rpx * FW) * uint32_t(ld) * 2u, dst + (wave + i * FW) * 1024);
+  };
+  auto dload = [&](int st) {
+    const int src = pr.nsrc > 1 ? seg & 1 : 0;
+    int64_t oa = 0, ob = 0;
+    if constexpr (F32) {
+      const int pp = plane_pair(pr.nsrc > 1 ? seg >> 1 : seg);
+      oa = (pp & 3) * pr.pa;
+      ob = (pp >> 2) * pr.pb;
+    }
+    const int k0 = kt * 64;
+    if (++kt == nkt) {
+      kt = 0;
+      ++seg;
+    }
+    if (wave >= FW) return;
+    const uint32_t sA = lds0 + uint32_t(st) * S::kStage, sB = sA + S::kStageA;
+    const char *A = pr.a[0] + oa, *B = pr.b[0] + ob;
+    if (src) {
+      A = pr.a[1] + oa;
+      B = pr.b[1] + ob;
+    }
+    if constexpr (AK) {
+      fetch_kn(A + int64_t(m0) * 2, pr.lda, BM * 2, k0, ((pr.m + 7) & ~7) - m0, sA, S::kLoadsA);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::kLoadsA; ++i)
+        fetch_rows(A + int64_t(m0) * pr.lda * 2, pr.lda, pr.m - m0, k0, sA, i, i * 8 * FW);
+    }
+    if constexpr (BK) {
+      fetch_kn(B + int64_t(n0) * 2, pr.ldb, BN * 2, k0, ((pr.n + 7) & ~7) - n0, sB, S::kLoadsB);
+    } else if constexpr (EPI == kAct) {
+      // rows 64 w .. 64 w + 31 of the stage: Wg's rows n0 + 32 w .., the next 32: Wu's
+      static_assert(FW == 4, "32 rows per half");
+      const char *U = pr.b[1] + ob;
+#pragma unroll
+      for (int i = 0; i < S::kLoadsB; ++i)
+        fetch_rows(((i & 1) ? U : B) + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB, i, (i >> 1) * 32);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::kLoadsB; ++i)
+        fetch_rows(B + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB, i, i * 8 * FW);
+    }
+  };
+
+  floatx16 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+#pragma unroll
+  for (int q = 0; q < NS - 1; ++q)
+    if (q < ns) dload(q);
+  for (int it = 0, st = 0; it < ns; ++it, st = st + 1 == NS ? 0 : st + 1) {
+    vm_wait_slabs<S::kLoadsA + S::kLoadsB, NS - 2>(min(NS - 2, ns - 1 - it));
+    __syncthreads();                 // slab `it` is published; the one before it is done
+    if (it + NS - 1 < ns) dload(st == 0 ? NS - 1 : st - 1);
+    const char *sA = smem + st * S::kStage, *sB = sA + S::kStageA;
+    bf16x8 fa[2][FM], fb[2][FN];
+    auto read = [&](int s, int slot) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[slot][i] = ffn_frag<AK, BM * 2>(sA, wm * S::WTM + i * 32, s, lane);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[slot][j] = ffn_frag<BK, BN * 2>(sB, wn * S::WTN + j * 32, s, lane);
+    };
+    read(0, 0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) read(s + 1, (s + 1) & 1);
+      // operands swapped: acc[i][j][4 g + q] = C[row lr of block i][column 32 j + 8 g + 4 lk + q]
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][j], fa[s & 1][i], acc[i][j], 0, 0, 0);
+    }
+    // the first k step's reads, then each step's MFMAs with the next step's
+    // reads spread among them
+    constexpr int kReads = FM * (AK ? 2 : 1) + FN * (BK ? 2 : 1), kMfma = FM * FN;
+    constexpr int kGroups = kReads < kMfma ? kReads : kMfma;
+    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int q = 0; q < kGroups; ++q) {
+        __builtin_amdgcn_sched_group_barrier(0x008, kMfma / kGroups, 0);
+        if (s < 3) __builtin_amdgcn_sched_group_barrier(0x100, kReads / kGroups, 0);
+      }
+  }
+  __syncthreads();                   // the epilogue reuses the stages
+
+  // Epilogue, per 32-row block of the wave tile: the fp32 sums go through the
+  // wave's own LDS area (one wave's LDS operations keep their order, so a
+  // wave-level barrier suffices), then each lane takes 8 consecutive columns.
+  float *ef = reinterpret_cast<float *>(smem) + wave * 32 * S::kPitch;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4v *>(ef + lr * S::kPitch + 32 * j + 8 * g + 4 * lk) =
+            float4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    __builtin_amdgcn_wave_barrier();
+    const int row0 = m0 + wm * S::WTM + i * 32;
+    constexpr int PC = EPI == kAct ? 4 : 8;               // 8-column pieces per row
+    constexpr int kTasks = 32 * PC / 64;
+    constexpr int kCopies = F32 && EPI != kStore ? 1 : kTasks;   // fp32 activations are long code
+#pragma unroll kCopies
+    for (int t = 0; t < kTasks; ++t) {
+      const int task = lane + 64 * t, rl = task / PC, cl = (task % PC) * 8;
+      const int row = row0 + rl;
+      float v[8];
+      auto staged = [&](int c, float (&o)[8]) {
+        const float4v e0 = *reinterpret_cast<const float4v *>(ef + rl * S::kPitch + c);
+        const float4v e1 = *reinterpret_cast<const float4v *>(ef + rl * S::kPitch + c + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = j < 4 ? e0[j & 3] : e1[j & 3];
+      };
+      staged(cl, v);
+      if constexpr (EPI == kAct) {
+        const int col = n0 + wn * 32 + cl;
+        float b[8], h[8];
+        staged(32 + cl, b);
+        if (row < pr.m && col < args.ldf) {
+          const int64_t at = int64_t(row) * args.ldf + col;
+          if (args.sa) {
+            store_kept<F32>(args.sa, args.ea, at, v);
+            store_kept<F32>(args.sb, args.eb, at, b);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float f, sl;
+            act_and_slope<F32>(args.act, v[j], f, sl);
+            h[j] = f * b[j];
+          }
+          store_planes<F32>(args.h + at * 2, args.plane, h);
+        }
+      } else if constexpr (EPI == kActBack) {
+        const int col = n0 + wn * 64 + cl;
+        if (row < pr.m && col < args.ldf) {
+          const int64_t at = int64_t(row) * args.ldf + col;
+          float a[8], b[8], h[8], da[8], db[8];
+          load_kept<F32>(args.sa, args.ea, at, a);
+          load_kept<F32>(args.sb, args.eb, at, b);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float f, sl;
+            act_and_slope<F32>(args.act, a[j], f, sl);
+            h[j] = f * b[j];
+            db[j] = v[j] * f;
+            da[j] = v[j] * b[j] * sl;
+          }
+          store_planes<F32>(args.h + at * 2, args.plane, h);
+          store_planes<F32>(args.da + at * 2, args.plane, da);
+          store_planes<F32>(args.db + at * 2, args.plane, db);
+        }
+      } else {
+        const int col = n0 + wn * 64 + cl;
+        if (row < pr.m && col < pr.n) {
+          if (pr.splits > 1) store_whole<true>(pr.part + (int64_t(split) * pr.m + row) * pr.ldp, col, v);
+          else store_some<F32>(pr.out, int64_t(row) * pr.ldo + col, pr.n - col, v);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+}  // namespace slorr

@@ -106,78 +106,6 @@ struct GemmShape {
   static constexpr int kSmem = (2 * kStage > kEpiAll) ? 2 * kStage : kEpiAll;
 };
 
-// Byte offset of 16-byte chunk `chunk` of LDS row `row`. The XOR key
-// (row & 7) ^ ((row >> 3) & 1) permutes the chunks so that (a) any 8
-// consecutive rows (one 8-lane phase of a 16-byte read with 32 banks) use 8
-// distinct chunk positions, and (b) any 16 consecutive rows (a 16-lane phase
-// with 64 banks, where rows of equal parity share a 128-byte bank half) use 8
-// distinct positions per parity.
-__device__ __forceinline__ int swz_key(int row) { return (row & 7) ^ ((row >> 3) & 1); }
-__device__ __forceinline__ int swz(int row, int chunk) { return row * 128 + ((chunk ^ swz_key(row)) << 4); }
-
-// 16 bytes per lane from a buffer straight into LDS: byte voff + soff of the
-// buffer (voff per lane, soff wave-uniform) lands at lds_base + 16 l
-// (lds_base wave-uniform, passed in m0). On the update tile's k loop this
-// form issues at a markedly lower cost than global_load_lds_dwordx4 with a
-// 64-bit address per lane; a load past the buffer's size returns zeros
-// instead of faulting. Device pass only: the host pass of the single-source
-// build just needs the kernel's stub.
-//
-// Issued through inline assembly: the compiler then does not track these LDS
-// writes and puts no wait for them before later LDS reads (it cannot tell
-// that those read the other stage). Completion is the caller's job: each
-// k-slab is waited for by count (s_waitcnt vmcnt) before the block barrier
-// that publishes it.
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ i32x4 buffer_rsrc(const void *base, uint32_t bytes) {
-  const uint64_t b = uint64_t(uintptr_t(base));
-  i32x4 r;
-  r[0] = __builtin_amdgcn_readfirstlane(int(uint32_t(b)));
-  r[1] = __builtin_amdgcn_readfirstlane(int(uint32_t(b >> 32) & 0xffffu));   // stride 0
-  r[2] = __builtin_amdgcn_readfirstlane(int(bytes));                        // size in bytes
-  r[3] = 0x00020000;                                                         // raw 32-bit dwords
-  return r;
-}
-__device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds_base) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const uint32_t m = __builtin_amdgcn_readfirstlane(lds_base);
-  const uint32_t so = __builtin_amdgcn_readfirstlane(soff);
-  asm volatile("buffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(m), "v"(voff), "s"(rsrc), "s"(so) : "memory");
-#else
-  (void)rsrc;
-  (void)voff;
-  (void)soff;
-  (void)lds_base;
-#endif
-}
-__device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uint32_t soff, void *lds_base) {
-  buffer_load_lds16(rsrc, voff, soff, uint32_t(uintptr_t(lds_base)));
-}
-
-// Transposing LDS read of 16-bit values (ds_read_b64_tr_b16). Within each
-// group of 16 lanes, lane s gives the address of 4 consecutive values: row
-// s / 4, columns 4 (s % 4) .. 4 (s % 4) + 3 of a 4 x 16 block; lane j then
-// holds column j of the block, element i from row i.
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ half4 lds_read_tr16(const void *lds) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  typedef __attribute__((__vector_size__(4 * sizeof(__fp16)))) __fp16 fp16x4;
-  typedef __attribute__((address_space(3))) fp16x4 lds_fp16x4;
-  const fp16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_fp16x4 *)(lds));
-  return __builtin_bit_cast(half4, v);
-#else
-  (void)lds;
-  return half4{};
-#endif
-}
-
-// Byte offset of 16-byte chunk `chunk` of k-row `row`
-// of a [k][n] operand stage (rows of `pitch` bytes). The key 4 (row & 3)
-// spreads the 4 rows x 4 chunks that one half-wave reads with a transposing
-// read (rows r..r+3 of a 16-row step, 64 bytes each) over all 64 banks.
-__device__ __forceinline__ int kn_off(int row, int chunk, int pitch) {
-  return row * pitch + ((chunk ^ ((row & 3) << 2)) << 4);
-}
 
 // Wait until every global -> LDS load this wave issued has landed (the
 // compiler does not count them, see buffer_load_lds16); precedes the block barrier

@@ -97,43 +97,6 @@ __device__ __forceinline__ double trace_planes(const half8 (&p)[Iter<T>::kPlanes
   return t;
 }
 
-// LDS byte offset of a shared array. The fetches below take offsets, not
-// pointers: a generic pointer would be cast back to LDS with a null check.
-__device__ __forceinline__ uint32_t lds_offset(const char *smem) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return uint32_t(uintptr_t((const __attribute__((address_space(3))) char *)smem));
-#else
-  (void)smem;
-  return 0;
-#endif
-}
-
-// s_waitcnt vmcnt(N), the other counters left alone (gfx9 encoding).
-template <int N>
-__device__ __forceinline__ void vm_wait() {
-  static_assert(N >= 0 && N < 64, "vmcnt");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
-}
-
-// Wait until at most `ahead` (<= A) slabs of fetches, L instructions each,
-// issued by this wave are outstanding.
-template <int L, int A>
-__device__ __forceinline__ void vm_wait_slabs(int ahead) {
-  if constexpr (A >= 2) {
-    if (ahead >= 2) {
-      vm_wait<2 * L>();
-      return;
-    }
-  }
-  if constexpr (A >= 1) {
-    if (ahead >= 1) {
-      vm_wait<L>();
-      return;
-    }
-  }
-  vm_wait<0>();
-}
-
 // The MFMAs of one 16-deep k step of a wave tile, operands swapped (the n
 // operand first): acc[i][j][4 g + q] = C[row lr of 32-row block i][column
 // 32 j + 8 g + 4 lk + q] of the wave tile. Split: the small cross terms

@@ -39,38 +39,11 @@
 #include <string>
 #include <type_traits>
 
+#include "device.hpp"
 #include "kernels.hpp"
 #include "layout.hpp"
 
 namespace slorr {
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef float float4v __attribute__((ext_vector_type(4)));
-typedef float float2v __attribute__((ext_vector_type(2)));
-typedef uint16_t bf16_t;
-
-// ------------------------------------------------------------------ helpers
-
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(bf16_t v) { return __uint_as_float(uint32_t(v) << 16); }
-__device__ __forceinline__ float to_f(_Float16 v) { return float(v); }
-
-// fp32 -> bf16 with round to nearest, ties to even (a NaN stays a quiet NaN):
-// add half an ulp of the bf16 result, minus one when the kept part is even,
-// then truncate.
-__device__ __forceinline__ bf16_t f32_to_bf16(float x) {
-  uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return bf16_t((u >> 16) | 0x40u);
-  u += 0x7fffu + ((u >> 16) & 1u);
-  return bf16_t(u >> 16);
-}
-
-template <typename T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ _Float16 from_f<_Float16>(float v) { return _Float16(v); }
-template <> __device__ __forceinline__ bf16_t from_f<bf16_t>(float v) { return f32_to_bf16(v); }
 
 // Sum over the NT threads of a block: butterfly within each wave, then the
 // per-wave sums in wave order. Fixed order, so bitwise reproducible. The
@@ -155,19 +128,6 @@ __device__ __forceinline__ void put8(T *p, int n, const float (&v)[8]) {
   }
 }
 
-// The full-tile path of the tile kernels below: 16-byte accesses known to be
-// aligned and in bounds, issued as global-memory instructions with no branch
-// between them, so that all of a thread's loads are in flight together (the
-// weight and gradient pointers come from a device table: left to itself the
-// compiler cannot tell their address space and emits flat accesses).
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ u32x4 gload16(const void *p) {
-  return *(const __attribute__((address_space(1))) u32x4 *)p;
-}
-__device__ __forceinline__ void gstore16(void *p, u32x4 v) { *(__attribute__((address_space(1))) u32x4 *)p = v; }
-__device__ __forceinline__ u32x4 gload16_stream(const void *p) {
-  return __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4 *)p);
-}
 
 // 8 consecutive values, 16-byte aligned and all in bounds, as floats.
 template <typename T>
