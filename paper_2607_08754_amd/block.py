@@ -23,6 +23,7 @@ the offset once per step, by more than its largest site.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import List, Optional, Tuple
 
@@ -73,8 +74,19 @@ def _rows(t: torch.Tensor, dim: int) -> Tuple[torch.Tensor, int]:
     return m, ld if n > 1 else dim
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _device(t: torch.Tensor):
+    """t's device as the current one (nothing to do where it is)."""
+    return _HERE if torch.cuda.current_device() == t.device.index else torch.cuda.device(t.device)
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # current_stream() without its Stream object
+
+
 def _stream(t: torch.Tensor) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return _raw_stream(t.device.index) if _raw_stream else torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -93,7 +105,7 @@ def _ffn_block(x, ldx, w_gate, act, lddy=0):
 
 def _ffn_forward(x, ldx, w_gate, w_up, w_down, act, keep):
     """y (tokens, dim) and, with keep, the state of the backward pass."""
-    with torch.cuda.device(x.device):
+    with _device(x):
         d = _ffn_block(x, ldx, w_gate, act)
         st, ws = ctypes.c_size_t(), ctypes.c_size_t()
         check(lib().slorr_ffn_sizes(d, st, ws, None), "slorr_ffn_sizes")
@@ -120,7 +132,7 @@ class _GatedFfn(torch.autograd.Function):
     def backward(ctx, dy):
         x, w_gate, w_up, w_down, state = ctx.saved_tensors
         need = ctx.needs_input_grad
-        with torch.cuda.device(x.device):
+        with _device(x):
             dy, lddy = _rows(dy, x.shape[1])
             d = _ffn_block(x, ctx.ldx, w_gate, ctx.act, lddy)
             ws = ctypes.c_size_t()
@@ -166,7 +178,7 @@ _JOIN = ("x", "f", "post_weight", "post_bias", "gate", "scale", "pre_weight", "p
 def _join_run(d, tensors, rng, want_y):
     """The forward call on laid-out inputs: y and z (None where absent)."""
     x = tensors[0]
-    with torch.cuda.device(x.device):
+    with _device(x):
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
         z = torch.empty(x.shape, dtype=x.dtype, device=x.device) if d.flags & _lib.JOIN_PRE else None
         check(lib().slorr_join_forward(d, _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
@@ -198,7 +210,7 @@ class _Join(torch.autograd.Function):
         d, x = ctx.d, laid[0]
         if all(t is None for t in douts):
             return (None,) * (2 + len(laid))
-        with torch.cuda.device(x.device):
+        with _device(x):
             douts = [None if t is None else _dense(t, x.shape[1]) for t in douts]
             dy = douts[0] if laid[1] is not None else None
             dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
@@ -325,7 +337,7 @@ def block_join(x: torch.Tensor, f: torch.Tensor, *, post: Optional[bool] = None,
 # ------------------------------------------------------------------ dropout
 
 def _dropout_run(x: torch.Tensor, p: float, rng, site: int) -> torch.Tensor:
-    with torch.cuda.device(x.device):
+    with _device(x):
         x = x.contiguous()
         if x.data_ptr() % 16:
             x = x.clone()

@@ -20,24 +20,47 @@ void check(hipError_t e, const char *what) {
 }
 
 // rows x cols values -> bf16 rows of ld numbers, zero padded (F32: three planes).
+// A call's operands go in one launch, one grid row each. Rows need no 16-byte
+// alignment: the memory system takes 16-byte loads at any multiple of an element.
+struct Lay {
+  const void *src;
+  char *dst;
+  int64_t rows, lds, plane;
+  int32_t cols, ld;
+};
+struct LayArgs {
+  Lay job[5];
+};
 template <bool F32>
-__global__ __launch_bounds__(256) void k_planes(const void *src, int64_t rows, int32_t cols, int64_t lds, char *dst,
-                                                int32_t ld, int64_t plane) {
+__global__ __launch_bounds__(256) void k_planes(LayArgs args) {
   using T = typename std::conditional<F32, float, uint16_t>::type;
-  const int pieces = ld >> 3;
-  const int64_t total = rows * pieces;
+  typedef u32x4 u32x4_any __attribute__((aligned(2)));
+  Lay a = args.job[0];
+#pragma unroll
+  for (int i = 1; i < 5; ++i)
+    if (int(blockIdx.y) == i) a = args.job[i];
+  const int pieces = a.ld >> 3;
+  const int64_t total = a.rows * pieces;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
     const int64_t r = i / pieces;
     const int c = int(i - r * pieces) * 8;
-    const T *p = static_cast<const T *>(src) + r * lds + c;
+    const T *p = static_cast<const T *>(a.src) + r * a.lds + c;
     float v[8];
-    if (c + 8 <= cols && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-      load_whole<F32>(p, 0, v);
+    if (c + 8 <= a.cols) {
+      const __attribute__((address_space(1))) u32x4_any *q = (const __attribute__((address_space(1))) u32x4_any *)p;
+      if constexpr (F32) {
+        const u32x4 q0 = q[0], q1 = q[1];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j < 4 ? q0[j & 3] : q1[j & 3]);
+      } else {
+        *reinterpret_cast<u32x4 *>(a.dst + (r * a.ld + c) * 2) = q[0];
+        continue;
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_f(p[j]) : 0.0f;
+      for (int j = 0; j < 8; ++j) v[j] = c + j < a.cols ? to_f(p[j]) : 0.0f;
     }
-    store_planes<F32>(dst + (r * ld + c) * 2, plane, v);
+    store_planes<F32>(a.dst + (r * a.ld + c) * 2, a.plane, v);
   }
 }
 
@@ -97,19 +120,30 @@ struct Operand {
   int64_t ld, plane;
 };
 
+// The operands of a call, laid out in one launch.
 template <bool F32>
-Operand operand(const FfnShape &s, const void *src, int64_t rows, int32_t cols, int64_t lds, char *ws, size_t off,
-                hipStream_t st) {
-  if (off == kAbsent) return {static_cast<const char *>(src), lds, 0};
-  Operand o{ws + off, up8(cols), rows * up8(cols) * 2};
-  const int64_t n = rows * (o.ld / 8);
-  if (n) {
-    const uint32_t grid = uint32_t(std::min<int64_t>(cdiv(n, 256), 8 * kCus));
-    hipLaunchKernelGGL(k_planes<F32>, dim3(grid), dim3(256), 0, st, src, rows, cols, lds, ws + off, int32_t(o.ld), o.plane);
+struct Layer {
+  const FfnShape &s;
+  char *ws;
+  LayArgs args{};
+  int n = 0;
+  int64_t most = 0;
+  Operand add(const void *src, int64_t rows, int32_t cols, int64_t lds, size_t off) {
+    if (off == kAbsent) return {static_cast<const char *>(src), lds, 0};
+    const Operand o{ws + off, up8(cols), rows * up8(cols) * 2};
+    if (rows) {
+      args.job[n++] = {src, ws + off, rows, lds, o.plane, cols, int32_t(o.ld)};
+      most = std::max(most, rows * (o.ld / 8));
+    }
+    return o;
+  }
+  void run(hipStream_t st) const {
+    if (!n) return;
+    const dim3 grid(uint32_t(std::min<int64_t>(cdiv(most, 256), 8 * kCus)), uint32_t(n));
+    hipLaunchKernelGGL(k_planes<F32>, grid, dim3(256), 0, st, args);
     check(hipGetLastError(), "kernel launch");
   }
-  return o;
-}
+};
 
 FfnProb product(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, void *out, int64_t ldo) {
   FfnProb p{};
@@ -133,10 +167,12 @@ void forward(const FfnShape &s, const void *x, const void *wg, const void *wu, c
              char *ws, hipStream_t st) {
   const FfnLayout l = ffn_layout(s, false);
   const int64_t T = s.tokens;
-  const Operand X = operand<F32>(s, x, T, s.dim, s.ldx, ws, l.x, st);
-  const Operand G = operand<F32>(s, wg, s.inner, s.dim, s.dim, ws, l.wg, st);
-  const Operand U = operand<F32>(s, wu, s.inner, s.dim, s.dim, ws, l.wu, st);
-  const Operand D = operand<F32>(s, wd, s.dim, s.inner, s.inner, ws, l.wd, st);
+  Layer<F32> lay{s, ws};
+  const Operand X = lay.add(x, T, s.dim, s.ldx, l.x);
+  const Operand G = lay.add(wg, s.inner, s.dim, s.dim, l.wg);
+  const Operand U = lay.add(wu, s.inner, s.dim, s.dim, l.wu);
+  const Operand D = lay.add(wd, s.dim, s.inner, s.inner, l.wd);
+  lay.run(st);
   const Operand H{ws + l.h, s.ldf(), T * s.ldf() * 2};
   FfnArgs a{};
   a.nprob = 1;
@@ -157,14 +193,23 @@ void backward(const FfnShape &s, const void *dy, const void *x, const void *wg, 
               const void *state, void *dx, void *dwg, void *dwu, void *dwd, char *ws, hipStream_t st) {
   const FfnLayout l = ffn_layout(s, true);
   const int64_t T = s.tokens;
-  const Operand DY = operand<F32>(s, dy, T, s.dim, s.lddy, ws, l.dy, st);
+  const bool by_x = dwg || dwu;
+  Layer<F32> lay{s, ws};
+  Operand D{}, G{}, U{}, X{};
+  const Operand DY = lay.add(dy, T, s.dim, s.lddy, l.dy);
+  if (T) D = lay.add(wd, s.dim, s.inner, s.inner, l.wd);
+  if (T && dx) {
+    G = lay.add(wg, s.inner, s.dim, s.dim, l.wg);
+    U = lay.add(wu, s.inner, s.dim, s.dim, l.wu);
+  }
+  if (by_x) X = lay.add(x, T, s.dim, s.ldx, l.x);
+  lay.run(st);
   const int64_t plane = T * s.ldf() * 2;
   const Operand H{ws + l.h, s.ldf(), plane}, DA{ws + l.da, s.ldf(), plane}, DB{ws + l.db, s.ldf(), plane};
   FfnArgs a{};
   a.act = s.act;
   a.ldf = int32_t(s.ldf());
   if (T) {
-    const Operand D = operand<F32>(s, wd, s.dim, s.inner, s.inner, ws, l.wd, st);
     a.nprob = 1;
     a.p[0] = product(DY, D, T, s.inner, s.dim, nullptr, 0);
     state_parts(s, const_cast<void *>(state), a);
@@ -175,8 +220,6 @@ void backward(const FfnShape &s, const void *dy, const void *x, const void *wg, 
     launch_products<false, true, kActBack, F32>(a, st);
   }
   if (dx && T) {
-    const Operand G = operand<F32>(s, wg, s.inner, s.dim, s.dim, ws, l.wg, st);
-    const Operand U = operand<F32>(s, wu, s.inner, s.dim, s.dim, ws, l.wu, st);
     a.nprob = 1;
     a.p[0] = product(DA, G, T, s.dim, s.inner, dx, s.dim);
     a.p[0].a[1] = DB.p;
@@ -185,8 +228,6 @@ void backward(const FfnShape &s, const void *dy, const void *x, const void *wg, 
     launch_products<false, true, kStore, F32>(a, st);
   }
   if (dwg || dwu || dwd) {
-    Operand X{};
-    if (dwg || dwu) X = operand<F32>(s, x, T, s.dim, s.ldx, ws, l.x, st);
     a.nprob = 0;
     if (dwg) a.p[a.nprob++] = product(DA, X, s.inner, s.dim, T, dwg, s.dim);
     if (dwu) a.p[a.nprob++] = product(DB, X, s.inner, s.dim, T, dwu, s.dim);

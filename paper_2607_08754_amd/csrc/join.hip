@@ -60,99 +60,195 @@ __device__ __forceinline__ Rng load_rng(const int64_t *rng, int64_t site) {
   return {uint64_t(rng[0]), uint64_t(rng[1]) + uint64_t(site)};
 }
 
-// Bit j: element e + j is kept. Eight elements from a multiple of 8 on take one
-// generator block, others two.
-__device__ __forceinline__ uint32_t keep8(int64_t e, const Rng &r, uint32_t drop) {
-  uint32_t bits = 0, c[4];
+// Eight elements' factors, k where element e + j is kept and 0 elsewhere. drop16
+// is the threshold in the upper half of a word: the upper 16-bit number of a word
+// is compared in place, the lower one shifted up. A run of eight that does not
+// start at a multiple of 8 takes two generator blocks.
+__device__ __forceinline__ void keep8(int64_t e, const Rng &r, uint32_t drop16, float k, float (&m)[8]) {
+  uint32_t c[4];
   philox(uint64_t(e) >> 3, r.offset, r.key, c);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) bits |= uint32_t(((c[j >> 1] >> (16 * (j & 1))) & 0xffffu) >= drop) << j;
   const int s = int(e & 7);
   if (s) {
-    uint32_t next = 0;
-    philox((uint64_t(e) >> 3) + 1, r.offset, r.key, c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) next |= uint32_t(((c[j >> 1] >> (16 * (j & 1))) & 0xffffu) >= drop) << j;
-    bits = (bits | next << 8) >> s;
+    uint32_t n[4];
+    philox((uint64_t(e) >> 3) + 1, r.offset, r.key, n);
+    // the eight numbers from s on: four words first, then 16 bits at a time
+    const bool far = s & 4;
+    const uint64_t q0 = uint64_t(c[1]) << 32 | c[0], q1 = uint64_t(c[3]) << 32 | c[2];
+    const uint64_t q2 = uint64_t(n[1]) << 32 | n[0], q3 = uint64_t(n[3]) << 32 | n[2];
+    const uint64_t a0 = far ? q1 : q0, a1 = far ? q2 : q1, a2 = far ? q3 : q2;
+    const int b = 16 * (s & 3);
+    const uint64_t t0 = b ? a0 >> b | a1 << (64 - b) : a0, t1 = b ? a1 >> b | a2 << (64 - b) : a1;
+    c[0] = uint32_t(t0);
+    c[1] = uint32_t(t0 >> 32);
+    c[2] = uint32_t(t1);
+    c[3] = uint32_t(t1 >> 32);
   }
-  return bits;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[2 * i] = c[i] << 16 >= drop16 ? k : 0.0f;
+    m[2 * i + 1] = c[i] >= drop16 ? k : 0.0f;
+  }
 }
 
 // ------------------------------------------------------------------- accesses
 
-// 8 values from column c of a row (zeros past dim). whole: rows are 16-byte
-// aligned and dim is a multiple of 8.
+// 8 consecutive values as loaded. Rows need no 16-byte alignment: the memory
+// system takes 16-byte accesses at any multiple of the element.
 template <typename T>
-__device__ __forceinline__ void get(const T *row, int c, int dim, bool whole, float (&v)[8]) {
-  if (whole) {
-    if (c < dim) {
-      if constexpr (sizeof(T) == 2) {
-        const u32x4 q = gload16(row + c);
+struct Raw {
+  u32x4 q[sizeof(T) / 2];
+};
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
+#define SLORR_GLOBAL __attribute__((address_space(1)))
+
+// The end of a row, n < 8 values, goes as runs of 4, 2 and 1: three accesses with
+// one address between them (a load and a store per value cost these kernels 50
+// registers, and with them half of their waves).
+template <typename T>
+__device__ __forceinline__ Raw<T> get(const T *row, int c, int dim) {
+  Raw<T> r;
+  if (c + 8 <= dim) {
+    const SLORR_GLOBAL u32x4_any *p = (const SLORR_GLOBAL u32x4_any *)(row + c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j & 1 ? q[j >> 1] & 0xffff0000u : q[j >> 1] << 16);
-      } else {
-        const u32x4 a = gload16(row + c), b = gload16(row + c + 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j < 4 ? a[j & 3] : b[j & 3]);
-      }
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    return;
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) r.q[i] = p[i];
+    return r;
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = c + j < dim ? to_f(row[c + j]) : 0.0f;
+  for (int i = 0; i < int(sizeof(T) / 2); ++i) r.q[i] = u32x4{0, 0, 0, 0};
+  const int n = dim - c;
+  if (n <= 0) return r;
+  const bool h4 = n & 4, h2 = n & 2;
+  const T *p2 = row + c + (n & 4), *p1 = row + c + (n & 6);
+  if constexpr (sizeof(T) == 2) {
+    u32x2_any a{0, 0};
+    uint32_t b = 0, d = 0;
+    if (h4) a = *(const SLORR_GLOBAL u32x2_any *)(row + c);
+    if (h2) b = *(const SLORR_GLOBAL u32_any *)p2;
+    if (n & 1) d = *(const SLORR_GLOBAL uint16_t *)p1;
+    const uint32_t lo = h2 ? b : d, hi = h2 ? d : 0u;
+    r.q[0] = u32x4{h4 ? a[0] : lo, h4 ? a[1] : hi, h4 ? lo : 0u, h4 ? hi : 0u};
+  } else {
+    u32x4 a{0, 0, 0, 0};
+    u32x2_any b{0, 0};
+    uint32_t d = 0;
+    if (h4) a = *(const SLORR_GLOBAL u32x4_any *)(row + c);
+    if (h2) b = *(const SLORR_GLOBAL u32x2_any *)p2;
+    if (n & 1) d = *(const SLORR_GLOBAL u32_any *)p1;
+    const uint32_t e0 = h2 ? b[0] : d, e1 = h2 ? b[1] : 0u, e2 = h2 ? d : 0u;
+    r.q[0] = h4 ? a : u32x4{e0, e1, e2, 0u};
+    if (h4) r.q[sizeof(T) / 2 - 1] = u32x4{e0, e1, e2, 0u};
+  }
+  return r;
 }
 
 template <typename T>
-__device__ __forceinline__ void put(T *row, int c, int dim, bool whole, const float (&v)[8]) {
-  if (whole) {
-    if (c >= dim) return;
-    if constexpr (sizeof(T) == 2) {
-      typedef float floatx8 __attribute__((ext_vector_type(8)));
-      typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-      floatx8 f;
+__device__ __forceinline__ void widen(const Raw<T> &r, float (&v)[8]) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = v[j];
-      gstore16(row + c, __builtin_bit_cast(u32x4, __builtin_convertvector(f, bf16x8)));
-    } else {
-      u32x4 a, b;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        a[j] = __float_as_uint(v[j]);
-        b[j] = __float_as_uint(v[4 + j]);
-      }
-      gstore16(row + c, a);
-      gstore16(row + c + 4, b);
-    }
-    return;
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (sizeof(T) == 2) v[j] = __uint_as_float(j & 1 ? r.q[0][j >> 1] & 0xffff0000u : r.q[0][j >> 1] << 16);
+    else v[j] = __uint_as_float(r.q[j >> 2][j & 3]);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (c + j < dim) row[c + j] = from_f<T>(v[j]);
 }
 
-// Sums of K values over the block, the result in every thread: butterfly within
-// each wave, then the waves' sums in wave order. sh: two buffers, used in turn
-// (a wave that writes one again has passed the barrier after the other's reads).
+template <typename T>
+__device__ __forceinline__ void put(T *row, int c, int dim, const float (&v)[8]) {
+  Raw<T> r;
+  if constexpr (sizeof(T) == 2) {
+    typedef float floatx8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    floatx8 f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = v[j];
+    r.q[0] = __builtin_bit_cast(u32x4, __builtin_convertvector(f, bf16x8));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.q[j >> 2][j & 3] = __float_as_uint(v[j]);
+  }
+  if (c + 8 <= dim) {
+    SLORR_GLOBAL u32x4_any *p = (SLORR_GLOBAL u32x4_any *)(row + c);
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) p[i] = r.q[i];
+    return;
+  }
+  const int n = dim - c;
+  if (n <= 0) return;
+  const bool h4 = n & 4, h2 = n & 2;
+  T *p2 = row + c + (n & 4), *p1 = row + c + (n & 6);
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t lo = h4 ? r.q[0][2] : r.q[0][0], hi = h4 ? r.q[0][3] : r.q[0][1];
+    if (h4) *(SLORR_GLOBAL u32x2_any *)(row + c) = u32x2_any{r.q[0][0], r.q[0][1]};
+    if (h2) *(SLORR_GLOBAL u32_any *)p2 = lo;
+    if (n & 1) *(SLORR_GLOBAL uint16_t *)p1 = uint16_t(h2 ? hi : lo);
+  } else {
+    const u32x4 e = h4 ? r.q[sizeof(T) / 2 - 1] : r.q[0];
+    if (h4) *(SLORR_GLOBAL u32x4_any *)(row + c) = r.q[0];
+    if (h2) *(SLORR_GLOBAL u32x2_any *)p2 = u32x2_any{e[0], e[1]};
+    if (n & 1) *(SLORR_GLOBAL u32_any *)p1 = h2 ? e[2] : e[0];
+  }
+}
+
+// NV pieces of 8 columns per thread, as fp32.
+template <int NV>
+struct Row {
+  float v[NV][8];
+};
+__device__ __forceinline__ int column(int v) { return (v * int(blockDim.x) + int(threadIdx.x)) * 8; }
+
+template <typename T>
+__device__ __forceinline__ void vector8(const void *p, int c, int dim, float none, float (&o)[8]) {
+  if (p) {
+    widen<T>(get(static_cast<const T *>(p), c, dim), o);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = none;
+  }
+}
+
+// The sum over a wave, in every lane: within a row of 16 lanes by data-parallel
+// moves, then across rows by the lane swaps.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_total(float v) {
+  v += dpp<0xB1>(v);                       // quad_perm [1, 0, 3, 2]
+  v += dpp<0x4E>(v);                       // quad_perm [2, 3, 0, 1]
+  v += dpp<0x141>(v);                      // row_half_mirror
+  v += dpp<0x140>(v);                      // row_mirror
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Sums over the block, the result in every thread: each wave's total, then the
+// waves' in order. Two buffers, used in turn: a wave that writes one again has
+// passed the barrier after the other's reads. Entries of waves that the block
+// does not have hold zeros.
+struct RowSums {
+  float v[2][2][8];
+};
+__device__ __forceinline__ void row_sums_init(RowSums &sh) {
+  if (threadIdx.x < 32) (&sh.v[0][0][0])[threadIdx.x] = 0.0f;
+  __syncthreads();
+}
 template <int K>
-__device__ __forceinline__ void row_sum(float (&v)[K], float (*sh)[8][K], int &turn) {
+__device__ __forceinline__ void row_sum(float (&p)[K], RowSums &sh, int &turn) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
-  const int waves = int(blockDim.x) >> 6;
-  if (waves == 1) return;
+  for (int k = 0; k < K; ++k) p[k] = wave_total(p[k]);
+  if (blockDim.x == 64) return;
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int k = 0; k < K; ++k) sh[turn][threadIdx.x >> 6][k] = v[k];
+    for (int k = 0; k < K; ++k) sh.v[turn][k][threadIdx.x >> 6] = p[k];
   __syncthreads();
+  const float4v *s = reinterpret_cast<const float4v *>(&sh.v[turn][0][0]);
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = 0.0f;
-  for (int w = 0; w < waves; ++w)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += sh[turn][w][k];
+  for (int k = 0; k < K; ++k) {
+    const float4v a = s[2 * k], b = s[2 * k + 1];
+    p[k] = ((a[0] + a[1]) + (a[2] + a[3])) + ((b[0] + b[1]) + (b[2] + b[3]));
+  }
   turn ^= 1;
 }
 
@@ -165,300 +261,460 @@ struct JoinArgs {
   float *part;                                  // [5][blocks][ldp]: w1, b1, scale, w2, b2; null: none wanted
   float *gpart;                                 // [blocks][ldp]; null: dgate is written directly
   int64_t rows, ldx, ldf, ldg, gate_rows, gate_run;   // gate_run: rows per gate row
+  int64_t per_block;                            // forward: rows per block
   int64_t groups, rpg, gpb, parts, rpp;         // JoinCut
   int64_t site;
   int32_t dim, ldp, layer, post, pre;
-  uint32_t drop;
-  float eps, alpha, keep;                       // keep: 1 / (1 - p')
-  int32_t wx, wf, wg, wd;                       // whole (see get): x, f, gate, contiguous tensors
+  uint32_t drop16;                              // threshold in a word's upper half; 0: keep all
+  float eps, inv, k;                            // inv: 1 / dim; k: alpha / (1 - p')
 };
 
-// The normalised row in place; returns r.
+// t - mu in place; columns past dim become zero.
 template <int NV>
-__device__ __forceinline__ float normalise(float (&t)[NV][8], const JoinArgs &a, float (*sh)[8][2], int &turn) {
-  const float inv = 1.0f / float(a.dim);
-  float q[2] = {0.0f, 0.0f};
+__device__ __forceinline__ void subtract_mean(Row<NV> &t, float mu, int dim) {
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t.v[v][j] = column(v) + j < dim ? t.v[v][j] - mu : 0.0f;
+}
+
+// mu out of t, and r of the norm; t^ is r t.
+template <int NV>
+__device__ __forceinline__ float norm_of(Row<NV> &t, const JoinArgs &a, RowSums &sh, int &turn) {
+  float p[1];
   if (a.layer) {
+    p[0] = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) q[0] += t[v][j];
-    row_sum<2>(q, sh, turn);
-    const float mu = q[0] * inv;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) t[v][j] = c + j < a.dim ? t[v][j] - mu : 0.0f;
-    }
-    q[0] = q[1] = 0.0f;
+      for (int j = 0; j < 8; ++j) p[0] += t.v[v][j];
+    row_sum<1>(p, sh, turn);
+    subtract_mean(t, p[0] * a.inv, a.dim);
   }
+  p[0] = 0.0f;
 #pragma unroll
   for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q[0] = fmaf(t[v][j], t[v][j], q[0]);
-  row_sum<2>(q, sh, turn);
-  const float r = 1.0f / sqrtf(fmaf(q[0], inv, a.eps));
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) t[v][j] *= r;
-  return r;
+    for (int j = 0; j < 8; ++j) p[0] = fmaf(t.v[v][j], t.v[v][j], p[0]);
+  row_sum<1>(p, sh, turn);
+  return __builtin_amdgcn_rsqf(fmaf(p[0], a.inv, a.eps));
 }
 
-// A norm's input gradient r (A - mean A - t^ mean(A t^)) in place of A.
-template <int NV>
-__device__ __forceinline__ void norm_back(float (&A)[NV][8], const float (&t)[NV][8], float r, const JoinArgs &a,
-                                          float (*sh)[8][2], int &turn) {
-  const float inv = 1.0f / float(a.dim);
-  float q[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      q[0] = fmaf(A[v][j], t[v][j], q[0]);
-      q[1] += A[v][j];
-    }
-  row_sum<2>(q, sh, turn);
-  const float mt = q[0] * inv, m = a.layer ? q[1] * inv : 0.0f;
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) A[v][j] = r * (A[v][j] - m - t[v][j] * mt);
-}
-
-template <typename T>
-__device__ __forceinline__ void vec(const void *p, int c, const JoinArgs &a, float none, float (&v)[8]) {
-  if (p) {
-    get(static_cast<const T *>(p), c, a.dim, a.wd, v);
+// The factors of a row's piece: k D.
+__device__ __forceinline__ void factors(const JoinArgs &a, const Rng &rng, int64_t row, int c, float k, float (&m)[8]) {
+  if (a.drop16) {
+    keep8(row * a.dim + c, rng, a.drop16, k, m);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = none;
+    for (int j = 0; j < 8; ++j) m[j] = k;
   }
 }
 
-// alpha D of 8 elements of a row
-__device__ __forceinline__ void factors(const JoinArgs &a, const Rng &rng, int64_t row, int c, float (&m)[8]) {
-  uint32_t bits = 0xffu;
-  if (a.drop) bits = keep8(row * a.dim + c, rng, a.drop);
-  const float k = a.drop ? a.alpha * a.keep : a.alpha;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) m[j] = (bits >> j) & 1u ? k : 0.0f;
+// A pointer whose loads are not moved: left to itself the compiler reads the
+// vectors once and holds them in registers over the loop over rows.
+__device__ __forceinline__ const void *unmoved(const void *p) {
+  asm volatile("" : "+s"(p));
+  return p;
 }
 
+// s g w1 and s g b1 of a piece for a gate row (null: 1).
+template <typename T>
+__device__ __forceinline__ void product8(const JoinArgs &a, const T *gate, int v, float (&sgw)[8], float (&sgb)[8]) {
+  float w[8], b[8], s[8], g[8];
+  vector8<T>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
+  vector8<T>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
+  vector8<T>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
+  vector8<T>(unmoved(gate), column(v), a.dim, 1.0f, g);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    sgw[j] = s[j] * g[j] * w[j];
+    sgb[j] = s[j] * g[j] * b[j];
+  }
+}
 template <typename T, int NV>
+__device__ __forceinline__ void products(const JoinArgs &a, const T *gate, Row<NV> &sgw, Row<NV> &sgb) {
+#pragma unroll
+  for (int v = 0; v < NV; ++v) product8<T>(a, gate, v, sgw.v[v], sgb.v[v]);
+}
+
+// A block takes a run of rows, each thread NV pieces of 8 columns of a row; the
+// next row's loads are issued before the current row's sums, and the vectors'
+// products are formed once per gate row. What bounds these kernels is the
+// instructions of a row (the generator's share: 20 32 x 32 products and 60 others
+// per 8 elements) as much as HBM.
+template <typename T, int NV, bool BIAS>
 __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
-  __shared__ float sh[2][8][2];
+  __shared__ RowSums sh;
+  row_sums_init(sh);
   int turn = 0;
-  const Rng rng = a.drop ? load_rng(a.rng, a.site) : Rng{};
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    float y[NV][8];
+  const Rng rng = a.drop16 ? load_rng(a.rng, a.site) : Rng{};
+  const int64_t r0 = blockIdx.x * a.per_block, r1 = min(a.rows, r0 + a.per_block);
+  Raw<T> nx[NV], nf[NV];
+  auto fetch = [&](int64_t row) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      get(static_cast<const T *>(a.x) + row * a.ldx, (v * int(blockDim.x) + int(threadIdx.x)) * 8, a.dim, a.wx, y[v]);
+    for (int v = 0; v < NV; ++v) {
+      nx[v] = get(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
+      if (a.f) nf[v] = get(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
+    }
+  };
+  if (r0 < r1) fetch(r0);
+  Row<NV> sgw, sgb, w2, b2;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    vector8<T>(a.w2, column(v), a.dim, 1.0f, w2.v[v]);
+    if constexpr (BIAS) vector8<T>(a.b2, column(v), a.dim, 0.0f, b2.v[v]);
+  }
+  int64_t gate_row = a.gate ? r0 / a.gate_run : 0, gate_end = a.gate ? (gate_row + 1) * a.gate_run : a.rows;
+  if (a.f && r0 < r1)
+    products<T>(a, a.gate ? static_cast<const T *>(a.gate) + gate_row * a.ldg : nullptr, sgw, sgb);
+#pragma unroll 1
+  for (int64_t row = r0; row < r1; ++row) {
+    if (a.f && row == gate_end) {
+      ++gate_row;
+      gate_end += a.gate_run;
+      products<T>(a, static_cast<const T *>(a.gate) + gate_row * a.ldg, sgw, sgb);
+    }
+    Row<NV> y, u;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      widen<T>(nx[v], y.v[v]);
+      if (a.f) widen<T>(nf[v], u.v[v]);
+    }
+    if (row + 1 < r1) fetch(row + 1);
     if (a.f) {
-      float u[NV][8];
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-        get(static_cast<const T *>(a.f) + row * a.ldf, (v * int(blockDim.x) + int(threadIdx.x)) * 8, a.dim, a.wf, u[v]);
-      if (a.post) normalise<NV>(u, a, sh, turn);
+      const float r = a.post ? norm_of<NV>(u, a, sh, turn) : 1.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-        float w[8], b[8], s[8], g[8], m[8];
-        vec<T>(a.w1, c, a, 1.0f, w);
-        vec<T>(a.b1, c, a, 0.0f, b);
-        vec<T>(a.scale, c, a, 1.0f, s);
-        if (a.gate) get(static_cast<const T *>(a.gate) + row / a.gate_run * a.ldg, c, a.dim, a.wg, g);
-        factors(a, rng, row, c, m);
+        float m[8];
+        factors(a, rng, row, column(v), a.k, m);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          y[v][j] = fmaf(m[j] * s[j] * (a.gate ? g[j] : 1.0f), fmaf(u[v][j], w[j], b[j]), y[v][j]);
+        for (int j = 0; j < 8; ++j) {
+          const float t = r * u.v[v][j];
+          y.v[v][j] = fmaf(m[j], BIAS ? fmaf(t, sgw.v[v][j], sgb.v[v][j]) : t * sgw.v[v][j], y.v[v][j]);
+        }
       }
     }
     if (a.y) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-        put(static_cast<T *>(a.y) + row * a.dim, (v * int(blockDim.x) + int(threadIdx.x)) * 8, a.dim, a.wd, y[v]);
+      for (int v = 0; v < NV; ++v) put(static_cast<T *>(a.y) + row * a.dim, column(v), a.dim, y.v[v]);
     }
     if (a.pre) {
-      // columns past dim hold zeros, but for a bias's sake: keep them out of the sums
-      normalise<NV>(y, a, sh, turn);
+      // (columns past dim hold zeros: the vectors and rows end there)
+      const float r = norm_of<NV>(y, a, sh, turn);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-        float w[8], b[8];
-        vec<T>(a.w2, c, a, 1.0f, w);
-        vec<T>(a.b2, c, a, 0.0f, b);
+        float ey[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[v][j] = fmaf(y[v][j], w[j], b[j]);
-        put(static_cast<T *>(a.z) + row * a.dim, c, a.dim, a.wd, y[v]);
+        for (int j = 0; j < 8; ++j) {
+          const float t = r * y.v[v][j];
+          y.v[v][j] = BIAS ? fmaf(t, w2.v[v][j], b2.v[v][j]) : t * w2.v[v][j];
+        }
+        put(static_cast<T *>(a.z) + row * a.dim, column(v), a.dim, y.v[v]);
       }
     }
   }
 }
 
+// Gate rows against a block's rows: one gate row (or none) for all of them, a
+// gate row for each, or several gate rows of several rows each.
+enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2 };
+
 // A block takes consecutive rows: whole groups (the rows of one gate row), or a
 // part of one group where there are fewer groups than blocks. Column sums stay
-// in registers over the block's rows and go to the block's partial row; the
-// gate's sum is flushed at each group's end.
-template <typename T, int NV>
-__global__ __launch_bounds__(512) void k_join_bwd(JoinArgs a) {
-  __shared__ float sh[2][8][2];
+// in registers over the block's rows and go to the block's partial row.
+//
+// The vectors leave the sums over rows: with M = D (kOneGate) or D g, P = sum dY
+// M f^ and Q = sum dY M, the sums of scale, post_weight and post_bias are k times
+// g (w1 P + b1 Q), s g P and s g Q (kOneGate's g; else 1), and one gate row's is
+// k s (w1 P + b1 Q). So a row adds to P, and Q where there are biases (BIAS), and
+// to dz y^ and dz; several gate rows add a sum of their own.
+//
+// A row has three block sums one after the other (RMS; LAYER five): the next
+// row is loaded before them, and the y norm's two sums share one.
+template <typename T, int NV, int MODE, bool BIAS>
+__global__ __launch_bounds__(512, NV == 1 && MODE == kOneGate && !BIAS && sizeof(T) == 2 ? 4 : 2)
+void k_join_bwd(JoinArgs a) {
+  __shared__ RowSums sh;
+  row_sums_init(sh);
   int turn = 0;
-  const Rng rng = a.drop ? load_rng(a.rng, a.site) : Rng{};
-  float sw1[NV][8] = {}, ss[NV][8] = {}, sg[NV][8] = {}, sw2[NV][8] = {};
-  // the biases' sums: with two pieces per thread in LDS, where the registers
-  // hold no more (each thread its own 16-byte slots)
-  constexpr bool kLds = NV > 1;
-  float sb1[NV][8] = {}, sb2[NV][8] = {};
-  __shared__ float4v bias_acc[kLds ? 4 * NV * 512 : 1];
-  auto bias_slot = [&](int which, int v, int half) -> float4v & {
-    return bias_acc[((which * NV + v) * 2 + half) * 512 + threadIdx.x];
+  const Rng rng = a.drop16 ? load_rng(a.rng, a.site) : Rng{};
+  // two pieces per thread: the biases' sums (beside a gate per row all sums) in LDS,
+  // each thread its own slots; the registers hold no more
+  constexpr bool kLds = NV > 1 && BIAS, kLdsP = kLds && MODE != kOneGate;
+  constexpr int kSlots = kLdsP ? 4 : kLds ? 2 : 0;
+  Row<NV> P = {}, Q = {}, sw2 = {}, sb2 = {}, sg = {};
+  __shared__ float4v sums[kLds ? kSlots * 2 * NV * 512 : 1];
+  auto slot = [&](int which, int v, int half) -> float4v & {
+    return sums[((which * NV + v) * 2 + half) * 512 + threadIdx.x];
   };
   if constexpr (kLds) {
 #pragma unroll
-    for (int i = 0; i < 2 * NV; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) bias_slot(i / NV, i % NV, h) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < kSlots * 2 * NV; ++i) slot(i / (2 * NV), (i >> 1) % NV, i & 1) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  auto bias_add = [&](int which, int v, const float (&x)[8], float (&acc)[8]) {
+  auto add = [&](int which, int v, const float (&x)[8], float (&acc)[8]) {
     if constexpr (kLds) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float4v t = bias_slot(which, v, h);
+        float4v t = slot(which, v, h);
 #pragma unroll
         for (int j = 0; j < 4; ++j) t[j] += x[4 * h + j];
-        bias_slot(which, v, h) = t;
+        slot(which, v, h) = t;
       }
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += x[j];
     }
   };
-  auto bias_get = [&](int which, int v, float (&acc)[8]) {
+  auto take = [&](int which, int v, float (&acc)[8]) {
     if constexpr (kLds) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = bias_slot(which, v, j >> 2)[j & 3];
+      for (int j = 0; j < 8; ++j) acc[j] = slot(which, v, j >> 2)[j & 3];
     }
   };
-  const bool each = a.gate && a.gate_run == 1;             // a gate row per row: no sum
+
   const int64_t blk = blockIdx.x;
   const int64_t g0 = a.parts > 1 ? blk / a.parts : blk * a.gpb;
   const int64_t g1 = a.parts > 1 ? g0 + 1 : min(a.groups, g0 + a.gpb);
-  for (int64_t grp = g0; grp < g1; ++grp) {
-    const int64_t r0 = grp * a.rpg + (a.parts > 1 ? (blk - g0 * a.parts) * a.rpp : 0);
-    const int64_t r1 = a.parts > 1 ? min(r0 + a.rpp, (grp + 1) * a.rpg) : r0 + a.rpg;
-    for (int64_t row = r0; row < r1; ++row) {
-      float y[NV][8], u[NV][8], d[NV][8];                  // y, then y^; f, then f^; dY
-      float r1f = 1.0f, r2 = 1.0f;
+  const int64_t r0 = g0 * a.rpg + (a.parts > 1 ? (blk - g0 * a.parts) * a.rpp : 0);
+  const int64_t r1 = a.parts > 1 ? min(r0 + a.rpp, g1 * a.rpg) : g1 * a.rpg;
+  int64_t gate_row = MODE == kEachRow ? r0 : MODE == kGroups ? g0 : a.gate && r0 < r1 ? r0 / a.gate_run : 0;
+  int64_t group_end = MODE == kGroups ? (g0 + 1) * a.rpg : 0;
+  const T *gate0 = MODE == kOneGate && a.gate ? static_cast<const T *>(a.gate) + gate_row * a.ldg : nullptr;
+  Raw<T> nx[NV], nf[NV], nd[NV], nz[NV], ng[NV];
+  // two pieces per thread: no loads ahead, each operand not before it is needed,
+  // the vectors' products and the dropout factors formed at each use
+  constexpr bool kAhead = NV == 1;
+  auto fetch_dy = [&](int64_t row) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-        get(static_cast<const T *>(a.x) + row * a.ldx, c, a.dim, a.wx, y[v]);
-        if (a.f) get(static_cast<const T *>(a.f) + row * a.ldf, c, a.dim, a.wf, u[v]);
-        if (a.dy) get(static_cast<const T *>(a.dy) + row * a.dim, c, a.dim, a.wd, d[v]);
-        else
+    for (int v = 0; v < NV; ++v)
+      if (a.dy) nd[v] = get(static_cast<const T *>(a.dy) + row * a.dim, column(v), a.dim);
+  };
+  auto fetch_gate = [&](int64_t gr) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) d[v][j] = 0.0f;
-      }
-      if (a.f && a.post) r1f = normalise<NV>(u, a, sh, turn);
-      if (a.pre && a.dz) {
-        float A[NV][8];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-          get(static_cast<const T *>(a.dz) + row * a.dim, c, a.dim, a.wd, A[v]);
-          if (a.f) {
-            float w[8], b[8], s[8], g[8], m[8];
-            vec<T>(a.w1, c, a, 1.0f, w);
-            vec<T>(a.b1, c, a, 0.0f, b);
-            vec<T>(a.scale, c, a, 1.0f, s);
-            if (a.gate) get(static_cast<const T *>(a.gate) + row / a.gate_run * a.ldg, c, a.dim, a.wg, g);
-            factors(a, rng, row, c, m);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              y[v][j] = fmaf(m[j] * s[j] * (a.gate ? g[j] : 1.0f), fmaf(u[v][j], w[j], b[j]), y[v][j]);
-          }
-        }
-        r2 = normalise<NV>(y, a, sh, turn);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          float w[8];
-          vec<T>(a.w2, (v * int(blockDim.x) + int(threadIdx.x)) * 8, a, 1.0f, w);
-          bias_add(1, v, A[v], sb2[v]);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            sw2[v][j] = fmaf(A[v][j], y[v][j], sw2[v][j]);
-            A[v][j] *= w[j];
-          }
-        }
-        norm_back<NV>(A, y, r2, a, sh, turn);
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) d[v][j] += A[v][j];
-      }
-      if (a.dx) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-          put(static_cast<T *>(a.dx) + row * a.dim, (v * int(blockDim.x) + int(threadIdx.x)) * 8, a.dim, a.wd, d[v]);
-      }
-      if (!a.f) continue;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-        float w[8], b[8], s[8], g[8], m[8], dg[8], du[8];
-        vec<T>(a.w1, c, a, 1.0f, w);
-        vec<T>(a.b1, c, a, 0.0f, b);
-        vec<T>(a.scale, c, a, 1.0f, s);
-        if (a.gate) get(static_cast<const T *>(a.gate) + row / a.gate_run * a.ldg, c, a.dim, a.wg, g);
-        factors(a, rng, row, c, m);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float gj = a.gate ? g[j] : 1.0f, dm = d[v][j] * m[j];
-          const float t = dm * fmaf(u[v][j], w[j], b[j]);
-          ss[v][j] = fmaf(t, gj, ss[v][j]);
-          dg[j] = t * s[j];
-          sg[v][j] += dg[j];
-          du[j] = dm * s[j] * gj;
-          sw1[v][j] = fmaf(du[j], u[v][j], sw1[v][j]);
-          d[v][j] = du[j] * w[j];
-        }
-        bias_add(0, v, du, sb1[v]);
-        if (each && a.dgate) put(static_cast<T *>(a.dgate) + row * a.dim, c, a.dim, a.wd, dg);
-      }
-      if (a.df) {
-        if (a.post) norm_back<NV>(d, u, r1f, a, sh, turn);
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-          put(static_cast<T *>(a.df) + row * a.dim, (v * int(blockDim.x) + int(threadIdx.x)) * 8, a.dim, a.wd, d[v]);
-      }
-    }
-    if (a.dgate && !each) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
-        if (a.gpart) put(a.gpart + blk * a.ldp, c, a.ldp, true, sg[v]);
-        else put(static_cast<T *>(a.dgate) + grp * a.dim, c, a.dim, a.wd, sg[v]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sg[v][j] = 0.0f;
-      }
-    }
-  }
-  if (a.part) {
-    const int64_t step = int64_t(gridDim.x) * a.ldp;
+    for (int v = 0; v < NV; ++v)
+      if constexpr (MODE != kOneGate) ng[v] = get(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
+  };
+  auto fetch = [&](int64_t row, int64_t gr) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * int(blockDim.x) + int(threadIdx.x)) * 8;
+      nx[v] = get(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
+      if (a.f) nf[v] = get(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
+      if (a.dz) nz[v] = get(static_cast<const T *>(a.dz) + row * a.dim, column(v), a.dim);
+      if constexpr (!kAhead && MODE != kOneGate)
+        ng[v] = get(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
+    }
+    if (kAhead) {
+      fetch_dy(row);
+      fetch_gate(gr);
+    }
+  };
+  Row<NV> sgw, sgb, w2;
+  if (kAhead && r0 < r1) fetch(r0, gate_row);
+  if (kAhead && a.f) products<T>(a, gate0, sgw, sgb);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) vector8<T>(a.w2, column(v), a.dim, 1.0f, w2.v[v]);
+  auto piece = [&](int v) {
+    if (!kAhead) {
+      __builtin_amdgcn_sched_barrier(0);
+      product8<T>(a, gate0, v, sgw.v[v], sgb.v[v]);
+    }
+  };
+
+#pragma unroll 1
+  for (int64_t row = r0; row < r1; ++row) {
+    // the next row's gate row
+    const bool turns = MODE == kEachRow || (MODE == kGroups && row + 1 == group_end);
+    const int64_t this_gate = gate_row;
+    if (turns) ++gate_row;
+    if (MODE == kGroups && turns) group_end += a.rpg;
+    if (!kAhead) fetch(row, this_gate);
+    Row<NV> y, u, d, e, m, g;
+    float rf = 1.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      widen<T>(nx[v], y.v[v]);
+      if (a.f) widen<T>(nf[v], u.v[v]);
+      if (a.dz) widen<T>(nz[v], e.v[v]);
+      if constexpr (MODE != kOneGate) widen<T>(ng[v], g.v[v]);
+    }
+    auto take_dy = [&]() {
+      if (!kAhead) {
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_dy(row);
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if (a.dy) {
+          widen<T>(nd[v], d.v[v]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d.v[v][j] = 0.0f;
+        }
+      }
+    };
+    if (kAhead) {
+      take_dy();
+      if (row + 1 < r1) fetch(row + 1, gate_row);
+    }
+    if (a.f) {
+      if (a.post) {
+        rf = norm_of<NV>(u, a, sh, turn);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) u.v[v][j] *= rf;
+      }
+      if (kAhead) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) factors(a, rng, row, column(v), 1.0f, m.v[v]);
+      }
+    }
+    if (a.dz) {
+      // y once more, then its norm's gradient; columns past dim hold zeros
+      if (a.f) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          piece(v);
+          if (!kAhead) factors(a, rng, row, column(v), 1.0f, m.v[v]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float km = MODE == kOneGate ? a.k * m.v[v][j] : a.k * m.v[v][j] * g.v[v][j];
+            y.v[v][j] = fmaf(km, BIAS ? fmaf(u.v[v][j], sgw.v[v][j], sgb.v[v][j]) : u.v[v][j] * sgw.v[v][j], y.v[v][j]);
+          }
+        }
+      }
+      if (!kAhead) __builtin_amdgcn_sched_barrier(0);
+      float p[2] = {0.0f, 0.0f}, mean = 0.0f;
+      if (a.layer) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p[0] += y.v[v][j];
+            p[1] = fmaf(e.v[v][j], w2.v[v][j], p[1]);
+          }
+        }
+        row_sum<2>(p, sh, turn);
+        subtract_mean(y, p[0] * a.inv, a.dim);
+        mean = p[1] * a.inv;
+        p[0] = p[1] = 0.0f;
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[0] = fmaf(y.v[v][j], y.v[v][j], p[0]);
+          p[1] = fmaf(e.v[v][j] * w2.v[v][j], y.v[v][j], p[1]);
+        }
+      }
+      row_sum<2>(p, sh, turn);
+      const float r = __builtin_amdgcn_rsqf(fmaf(p[0], a.inv, a.eps)), mt = p[1] * a.inv * r;
+      if (!kAhead) take_dy();
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float ey[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float t = r * y.v[v][j];
+          d.v[v][j] = fmaf(r, fmaf(-t, mt, fmaf(e.v[v][j], w2.v[v][j], -mean)), d.v[v][j]);
+          if constexpr (kLdsP) ey[j] = e.v[v][j] * t;
+          else sw2.v[v][j] = fmaf(e.v[v][j], t, sw2.v[v][j]);
+        }
+        if constexpr (kLdsP) add(3, v, ey, sw2.v[v]);
+        if constexpr (BIAS) add(1, v, e.v[v], sb2.v[v]);
+      }
+    }
+    if (!kAhead && !a.dz) take_dy();
+    if (a.dx) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) put(static_cast<T *>(a.dx) + row * a.dim, column(v), a.dim, d.v[v]);
+    }
+    if (!a.f) continue;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float dg[8], du[8];
+      piece(v);
+      if (!kAhead) factors(a, rng, row, column(v), 1.0f, m.v[v]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        d.v[v][j] *= m.v[v][j];                                  // dY D
+        if constexpr (MODE != kOneGate) {
+          const float t = a.k * d.v[v][j];
+          dg[j] = t * (BIAS ? fmaf(u.v[v][j], sgw.v[v][j], sgb.v[v][j]) : u.v[v][j] * sgw.v[v][j]);
+          if constexpr (MODE == kGroups) dg[j] = sg.v[v][j] += dg[j];
+          d.v[v][j] *= g.v[v][j];
+        }
+        if constexpr (kLdsP) du[j] = d.v[v][j] * u.v[v][j];
+        else P.v[v][j] = fmaf(d.v[v][j], u.v[v][j], P.v[v][j]);
+      }
+      if constexpr (BIAS) add(0, v, d.v[v], Q.v[v]);
+      if constexpr (kLdsP) add(2, v, du, P.v[v]);
+      // du w1 = k dY M s g w1
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d.v[v][j] *= a.k * sgw.v[v][j];
+      if constexpr (MODE != kOneGate) {
+        if (turns) {
+          if (a.dgate) put(static_cast<T *>(a.dgate) + this_gate * a.dim, column(v), a.dim, dg);
+          if constexpr (MODE == kGroups) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sg.v[v][j] = 0.0f;
+          }
+        }
+      }
+    }
+    if (a.df) {
+      if (a.post) {
+        float p[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p[0] = fmaf(d.v[v][j], u.v[v][j], p[0]);
+            p[1] += d.v[v][j];
+          }
+        row_sum<2>(p, sh, turn);
+        const float mt = p[0] * a.inv, mean = a.layer ? p[1] * a.inv : 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d.v[v][j] = rf * fmaf(-u.v[v][j], mt, d.v[v][j] - mean);
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) put(static_cast<T *>(a.df) + row * a.dim, column(v), a.dim, d.v[v]);
+    }
+  }
+
+  if (!a.part && !a.gpart) return;
+  const int64_t step = int64_t(gridDim.x) * a.ldp;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    float w[8], b[8], s[8], g[8], t1[8], t2[8], t3[8], dg[8];
+    take(0, v, Q.v[v]);
+    take(1, v, sb2.v[v]);
+    if constexpr (kLdsP) {
+      take(2, v, P.v[v]);
+      take(3, v, sw2.v[v]);
+    }
+    vector8<T>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
+    vector8<T>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
+    vector8<T>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
+    vector8<T>(unmoved(gate0), column(v), a.dim, 1.0f, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float q = a.k * (BIAS ? fmaf(w[j], P.v[v][j], b[j] * Q.v[v][j]) : w[j] * P.v[v][j]);
+      t1[j] = a.k * s[j] * g[j] * P.v[v][j];
+      t2[j] = a.k * s[j] * g[j] * Q.v[v][j];
+      t3[j] = g[j] * q;
+      dg[j] = s[j] * q;
+    }
+    if (MODE == kOneGate && a.gpart) put(a.gpart + blk * a.ldp, column(v), a.ldp, dg);
+    if (a.part) {
       float *p = a.part + blk * a.ldp;
-      bias_get(0, v, sb1[v]);
-      bias_get(1, v, sb2[v]);
-      put(p, c, a.ldp, true, sw1[v]);
-      put(p + step, c, a.ldp, true, sb1[v]);
-      put(p + 2 * step, c, a.ldp, true, ss[v]);
-      put(p + 3 * step, c, a.ldp, true, sw2[v]);
-      put(p + 4 * step, c, a.ldp, true, sb2[v]);
+      put(p, column(v), a.ldp, t1);
+      put(p + step, column(v), a.ldp, t2);
+      put(p + 2 * step, column(v), a.ldp, t3);
+      put(p + 3 * step, column(v), a.ldp, sw2.v[v]);
+      put(p + 4 * step, column(v), a.ldp, sb2.v[v]);
     }
   }
 }
@@ -509,18 +765,19 @@ __global__ __launch_bounds__(1024) void k_join_sum(SumArgs a) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_dropout(int64_t n, uint32_t drop, const int64_t *rng_p, int64_t site,
+__global__ __launch_bounds__(256) void k_dropout(int64_t n, uint32_t drop16, const int64_t *rng_p, int64_t site,
                                                  float keep, const T *x, T *y) {
   const Rng rng = load_rng(rng_p, site);
   const int64_t pieces = (n + 7) >> 3;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
     const int left = int(min(int64_t(8), n - i * 8));
-    float v[8];
-    get(x + i * 8, 0, left, left == 8, v);
-    const uint32_t bits = keep8(i * 8, rng, drop);
+    const Raw<T> r = get(x + i * 8, 0, left);
+    float v[8], m[8];
+    keep8(i * 8, rng, drop16, keep, m);
+    widen<T>(r, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (bits >> j) & 1u ? v[j] * keep : 0.0f;
-    put(y + i * 8, 0, left, left == 8, v);
+    for (int j = 0; j < 8; ++j) v[j] = m[j] != 0.0f ? v[j] * keep : 0.0f;
+    put(y + i * 8, 0, left, v);
   }
 }
 
@@ -556,17 +813,42 @@ JoinArgs join_args(const JoinShape &s, const slorr_join_tensors_t &t, const int6
   a.layer = s.layer;
   a.post = s.post;
   a.pre = s.pre;
-  a.drop = s.drop;
+  a.drop16 = s.drop << 16;
   a.eps = s.eps;
-  a.alpha = s.alpha;
-  a.keep = keep_factor(s.drop);
-  const int64_t per = s.dtype == SLORR_BF16 ? 8 : 4;       // elements per 16 bytes
-  const bool whole = s.dim % 8 == 0;
-  a.wd = whole;
-  a.wx = whole && s.ldx % per == 0;
-  a.wf = whole && s.ldf % per == 0;
-  a.wg = whole && s.ld_gate % per == 0;
+  a.inv = 1.0f / float(s.dim);
+  a.k = s.alpha * keep_factor(s.drop);
   return a;
+}
+
+template <typename T>
+void launch_forward(const JoinArgs &a, uint32_t grid, int threads, hipStream_t st) {
+  const bool bias = a.b1 || a.b2;
+  if (a.dim > 4096) {
+    if (bias) hipLaunchKernelGGL((k_join_fwd<T, 2, true>), dim3(grid), dim3(threads), 0, st, a);
+    else hipLaunchKernelGGL((k_join_fwd<T, 2, false>), dim3(grid), dim3(threads), 0, st, a);
+  } else {
+    if (bias) hipLaunchKernelGGL((k_join_fwd<T, 1, true>), dim3(grid), dim3(threads), 0, st, a);
+    else hipLaunchKernelGGL((k_join_fwd<T, 1, false>), dim3(grid), dim3(threads), 0, st, a);
+  }
+}
+
+template <typename T, int NV, int MODE>
+void launch_backward_as(const JoinArgs &a, int64_t blocks, hipStream_t st) {
+  const dim3 grid{uint32_t(blocks)}, block(join_threads(a.dim));
+  if (a.b1 || a.b2) hipLaunchKernelGGL((k_join_bwd<T, NV, MODE, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_join_bwd<T, NV, MODE, false>), grid, block, 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+}
+template <typename T, int NV>
+void launch_backward_of(const JoinArgs &a, int mode, int64_t blocks, hipStream_t st) {
+  if (mode == kEachRow) launch_backward_as<T, NV, kEachRow>(a, blocks, st);
+  else if (NV == 1 && mode == kGroups) launch_backward_as<T, 1, kGroups>(a, blocks, st);
+  else launch_backward_as<T, NV, kOneGate>(a, blocks, st);
+}
+template <typename T>
+void launch_backward(const JoinArgs &a, int mode, int64_t blocks, hipStream_t st) {
+  if (a.dim > 4096) launch_backward_of<T, 2>(a, mode, blocks, st);
+  else launch_backward_of<T, 1>(a, mode, blocks, st);
 }
 
 }  // namespace
@@ -577,7 +859,12 @@ JoinCut join_cut(const JoinShape &s) {
   const bool summed = s.gate_rows > 1 && s.gate_rows < s.rows;     // gate rows of several tokens each
   c.groups = summed ? s.gate_rows : 1;
   c.rows_per_group = s.rows / c.groups;
-  if (c.groups >= target) {
+  if (c.groups >= target && s.dim > 4096) {
+    // two pieces per thread leave no registers for a gate's own sums
+    c.parts = c.groups_per_block = 1;
+    c.rows_per_part = c.rows_per_group;
+    c.blocks = c.groups;
+  } else if (c.groups >= target) {
     c.groups_per_block = cdiv(c.groups, target);
     c.parts = 1;
     c.rows_per_part = c.rows_per_group;
@@ -603,15 +890,12 @@ void enqueue_join_forward(const JoinShape &s, const slorr_join_tensors_t &t, con
   JoinArgs a = join_args(s, t, rng);
   a.y = y;
   a.z = z;
-  const dim3 grid(uint32_t(std::min<int64_t>(s.rows, 16 * kCus))), block(join_threads(s.dim));
-  const bool two = s.dim > 4096;
-  if (s.dtype == SLORR_BF16) {
-    if (two) hipLaunchKernelGGL((k_join_fwd<bf16_t, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_join_fwd<bf16_t, 1>), grid, block, 0, st, a);
-  } else {
-    if (two) hipLaunchKernelGGL((k_join_fwd<float, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_join_fwd<float, 1>), grid, block, 0, st, a);
-  }
+  // as many blocks as the CUs hold at once (16 waves each), each a run of rows
+  const int threads = join_threads(s.dim);
+  a.per_block = std::max<int64_t>(1, cdiv(s.rows, kCus * (16 * 64 / threads)));
+  const uint32_t grid = uint32_t(cdiv(s.rows, a.per_block));
+  if (s.dtype == SLORR_BF16) launch_forward<bf16_t>(a, grid, threads, st);
+  else launch_forward<float>(a, grid, threads, st);
   check(hipGetLastError(), "kernel launch");
 }
 
@@ -641,20 +925,13 @@ void enqueue_join_backward(const JoinShape &s, const slorr_join_tensors_t &t, co
   const bool each = a.gate && a.gate_run == 1 && s.gate_rows == s.rows;
   // the gate's sums are joined afterwards where a gate row's tokens are spread
   // over blocks, and where there is no token to write them
-  const bool joined = g.gate && (!s.rows || (!each && c.parts > 1));
+  const bool joined = g.gate && (!s.rows || (!each && (c.parts > 1 || s.dim > 4096)));
   a.part = q.kinds ? w : nullptr;
   a.gpart = joined ? w + 5 * n : nullptr;
   if (s.rows) {
-    const dim3 grid{uint32_t(c.blocks)}, block(join_threads(s.dim));
-    const bool two = s.dim > 4096;
-    if (s.dtype == SLORR_BF16) {
-      if (two) hipLaunchKernelGGL((k_join_bwd<bf16_t, 2>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((k_join_bwd<bf16_t, 1>), grid, block, 0, st, a);
-    } else {
-      if (two) hipLaunchKernelGGL((k_join_bwd<float, 2>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((k_join_bwd<float, 1>), grid, block, 0, st, a);
-    }
-    check(hipGetLastError(), "kernel launch");
+    const int mode = each ? kEachRow : a.gate && c.groups > 1 && c.parts == 1 && s.dim <= 4096 ? kGroups : kOneGate;
+    if (s.dtype == SLORR_BF16) launch_backward<bf16_t>(a, mode, c.blocks, st);
+    else launch_backward<float>(a, mode, c.blocks, st);
   }
   const int64_t gates = joined ? (s.rows ? c.groups : s.gate_rows) : 0;
   if (!q.kinds && !gates) return;
@@ -688,12 +965,12 @@ void enqueue_dropout(int64_t n, int32_t dtype, uint32_t drop, const int64_t *rng
   if (dtype == SLORR_BF16) {
     const bf16_t *p = static_cast<const bf16_t *>(x);
     bf16_t *q = static_cast<bf16_t *>(y);
-    if (drop) hipLaunchKernelGGL(k_dropout<bf16_t>, grid, block, 0, st, n, drop, rng, site, keep_factor(drop), p, q);
+    if (drop) hipLaunchKernelGGL(k_dropout<bf16_t>, grid, block, 0, st, n, drop << 16, rng, site, keep_factor(drop), p, q);
     else hipLaunchKernelGGL(k_copy<bf16_t>, grid, block, 0, st, n, p, q);
   } else {
     const float *p = static_cast<const float *>(x);
     float *q = static_cast<float *>(y);
-    if (drop) hipLaunchKernelGGL(k_dropout<float>, grid, block, 0, st, n, drop, rng, site, keep_factor(drop), p, q);
+    if (drop) hipLaunchKernelGGL(k_dropout<float>, grid, block, 0, st, n, drop << 16, rng, site, keep_factor(drop), p, q);
     else hipLaunchKernelGGL(k_copy<float>, grid, block, 0, st, n, p, q);
   }
   check(hipGetLastError(), "kernel launch");

@@ -357,11 +357,13 @@ def test_join(B, S, D, kind, post, gate, scale, pre, p, dtype):
     _join_check(t, kw, dy, dz, dtype)
 
 
-@pytest.mark.parametrize("gate,B,S", [("batch", 1500, 2), ("batch", 5, 700), ("token", 30, 50), ("channel", 3, 1000),
-                                      ("batch", 1024, 1), ("batch", 1025, 3)])
-def test_join_cuts(gate, B, S):
-    """More gate rows than blocks, fewer, and one for all."""
-    t, kw, dy, dz = _join_case(B, S, 40, "f32", "rms", True, gate, True, True, 0.1)
+@pytest.mark.parametrize("gate,B,S,D,kind", [
+    ("batch", 1500, 2, 40, "rms"), ("batch", 1500, 2, 40, "layer"), ("batch", 5, 700, 40, "rms"), ("token", 30, 50, 40, "rms"),
+    ("channel", 3, 1000, 40, "layer"), ("batch", 1024, 1, 40, "rms"), ("batch", 1025, 3, 41, "rms"),
+    ("batch", 1030, 2, 4104, "layer"), ("batch", 3, 5, 4104, "layer")])
+def test_join_cuts(gate, B, S, D, kind):
+    """More gate rows than blocks, fewer, and one for all; rows of two pieces per thread."""
+    t, kw, dy, dz = _join_case(B, S, D, "f32", kind, True, gate, True, True, 0.1)
     _join_check(t, kw, dy, dz, "f32")
 
 
