@@ -41,32 +41,32 @@ _NORM = {"rms": _lib.RMS, "layer": _lib.LAYER}
 _MAX_STRIDE = (1 << 22) - 8
 
 
-def _check_first(x: torch.Tensor, name: str) -> int:
+def _check_first(x: torch.Tensor, name: str) -> None:
     if not isinstance(x, torch.Tensor) or x.dtype not in _DTYPE:
         raise ValueError(f"{name} must be a float32 or bfloat16 tensor")
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError(f"{name} must be on a GPU")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"{name} must have a last dimension of at least 1")
-    return _DTYPE[x.dtype]
 
 
-def _check_like(t: Optional[torch.Tensor], shape, x: torch.Tensor, name: str) -> None:
-    if t is None:
-        return
-    if tuple(t.shape) != tuple(shape) or t.dtype != x.dtype or t.device != x.device:
+def _check_like(t: torch.Tensor, shape, x: torch.Tensor, name: str) -> None:
+    if t.shape != shape or t.dtype != x.dtype or t.device != x.device:
         raise ValueError(f"{name} must be a {x.dtype} {tuple(shape)} tensor on {x.device}")
 
 
-def _check_vector(t, shape, x, name):
+def _check_dense(t: torch.Tensor, shape, x: torch.Tensor, name: str) -> None:
     _check_like(t, shape, x, name)
-    if t is not None and not t.is_contiguous():
+    if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
 
 
 def _rows(t: torch.Tensor, dim: int) -> Tuple[torch.Tensor, int]:
-    """t as rows of dim values, 16-byte aligned, and the stride of its rows."""
-    m = t if t.dim() == 2 else t.reshape(-1, dim)
+    """t's values as rows of dim at a fixed stride, 16-byte aligned: the tensor
+    to read (t itself where it is laid out so) and the stride."""
+    if t.is_contiguous():
+        return (t, dim) if t.data_ptr() % 16 == 0 else (t.clone(), dim)
+    m = t.reshape(-1, dim)
     n, ld = m.shape[0], m.stride(0)
     if (dim > 1 and m.stride(1) != 1) or (n > 1 and not dim <= ld <= _MAX_STRIDE) or m.data_ptr() % 16:
         m = m.clone(memory_format=torch.contiguous_format)
@@ -100,16 +100,17 @@ def _bytes(n: int, like: torch.Tensor) -> torch.Tensor:
 # ------------------------------------------------------------- feed-forward
 
 def _ffn_block(x, ldx, w_gate, act, lddy=0):
-    return _lib.Ffn(x.shape[0], w_gate.shape[1], w_gate.shape[0], _DTYPE[x.dtype], act, ldx, lddy)
+    inner, dim = w_gate.shape
+    return _lib.Ffn(x.numel() // dim, dim, inner, _DTYPE[x.dtype], act, ldx, lddy)
 
 
-def _ffn_forward(x, ldx, w_gate, w_up, w_down, act, keep):
-    """y (tokens, dim) and, with keep, the state of the backward pass."""
+def _ffn_forward(x, shape, ldx, w_gate, w_up, w_down, act, keep):
+    """y and, with keep, the state of the backward pass. x is laid out by _rows."""
     with _device(x):
         d = _ffn_block(x, ldx, w_gate, act)
         st, ws = ctypes.c_size_t(), ctypes.c_size_t()
         check(lib().slorr_ffn_sizes(d, st, ws, None), "slorr_ffn_sizes")
-        y = torch.empty((x.shape[0], x.shape[1]), dtype=x.dtype, device=x.device)
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
         state = _bytes(st.value, x) if keep else None
         work = _bytes(ws.value, x)
         check(lib().slorr_ffn_forward(d, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
@@ -121,11 +122,11 @@ def _ffn_forward(x, ldx, w_gate, w_up, w_down, act, keep):
 class _GatedFfn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, act):
-        rows, ldx = _rows(x, x.shape[-1])
-        y, state = _ffn_forward(rows, ldx, w_gate, w_up, w_down, act, True)
+        rows, ldx = _rows(x, w_gate.shape[1])
+        y, state = _ffn_forward(rows, x.shape, ldx, w_gate, w_up, w_down, act, True)
         ctx.act, ctx.ldx, ctx.shape = act, ldx, x.shape
         ctx.save_for_backward(rows, w_gate, w_up, w_down, state)
-        return y.view(x.shape)
+        return y
 
     @staticmethod
     @once_differentiable
@@ -133,18 +134,16 @@ class _GatedFfn(torch.autograd.Function):
         x, w_gate, w_up, w_down, state = ctx.saved_tensors
         need = ctx.needs_input_grad
         with _device(x):
-            dy, lddy = _rows(dy, x.shape[1])
+            dy, lddy = _rows(dy, w_gate.shape[1])
             d = _ffn_block(x, ctx.ldx, w_gate, ctx.act, lddy)
             ws = ctypes.c_size_t()
             check(lib().slorr_ffn_sizes(d, None, None, ws), "slorr_ffn_sizes")
-            grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if n else None
-                     for t, n in zip((x, w_gate, w_up, w_down), need)]
+            grads = [torch.empty(s, dtype=x.dtype, device=x.device) if n else None
+                     for s, n in zip((ctx.shape, w_gate.shape, w_up.shape, w_down.shape), need)]
             work = _bytes(ws.value, x)
             check(lib().slorr_ffn_backward(d, dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
                                            w_down.data_ptr(), state.data_ptr(), *map(_ptr, grads), work.data_ptr(),
                                            ws.value, _stream(x)), "slorr_ffn_backward")
-        if grads[0] is not None:
-            grads[0] = grads[0].view(ctx.shape)
         return (*grads, None)
 
 
@@ -162,46 +161,46 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     if w_gate.dim() != 2 or w_gate.shape[0] < 1:
         raise ValueError("w_gate must be a matrix of at least one row")
     inner = w_gate.shape[0]
-    for t, shape, name in ((w_gate, (inner, dim), "w_gate"), (w_up, (inner, dim), "w_up"), (w_down, (dim, inner), "w_down")):
-        _check_vector(t, shape, x, name)
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down)):
+    _check_dense(w_gate, (inner, dim), x, "w_gate")
+    _check_dense(w_up, (inner, dim), x, "w_up")
+    _check_dense(w_down, (dim, inner), x, "w_down")
+    if torch.is_grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad
+                                    or w_down.requires_grad):
         return _GatedFfn.apply(x, w_gate, w_up, w_down, _ACT[act])
     rows, ldx = _rows(x, dim)
-    return _ffn_forward(rows, ldx, w_gate, w_up, w_down, _ACT[act], False)[0].view(x.shape)
+    return _ffn_forward(rows, x.shape, ldx, w_gate, w_up, w_down, _ACT[act], False)[0]
 
 
 # --------------------------------------------------------------------- join
 
 _JOIN = ("x", "f", "post_weight", "post_bias", "gate", "scale", "pre_weight", "pre_bias")
+_VECTORS = (2, 3, 5, 6, 7)
 
 
-def _join_run(d, tensors, rng, want_y):
-    """The forward call on laid-out inputs: y and z (None where absent)."""
+def _join_run(d, shape, tensors, rng):
+    """The forward call on laid-out inputs: y (None without f) and z (None without PRE)."""
     x = tensors[0]
     with _device(x):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
-        z = torch.empty(x.shape, dtype=x.dtype, device=x.device) if d.flags & _lib.JOIN_PRE else None
+        y = None if tensors[1] is None else torch.empty(shape, dtype=x.dtype, device=x.device)
+        z = torch.empty(shape, dtype=x.dtype, device=x.device) if d.flags & _lib.JOIN_PRE else None
         check(lib().slorr_join_forward(d, _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
                                        _stream(x)), "slorr_join_forward")
     return y, z
 
 
 class _Join(torch.autograd.Function):
-    """forward(d, shapes, rng, *tensors): tensors are laid out by _join_inputs
-    in the order of _JOIN; d describes the call. Returns (y, z), or z alone
-    without f."""
+    """forward(d, rng, *tensors): d describes the call, tensors in the order of
+    _JOIN. Returns (y, z), or what there is of them."""
 
     @staticmethod
     def forward(ctx, d, rng, *tensors):
         laid = _join_layout(d, tensors)
-        y, z = _join_run(d, laid, rng, laid[1] is not None)
+        y, z = _join_run(d, tensors[0].shape, laid, rng)
         ctx.d = d
         ctx.shapes = [None if t is None else t.shape for t in tensors]
         ctx.save_for_backward(rng, *laid)
         ctx.set_materialize_grads(False)
-        shape = tensors[0].shape
-        outs = tuple(t.view(shape) for t in (y, z) if t is not None)
-        return outs if len(outs) > 1 else outs[0]
+        return (y, z) if y is not None and z is not None else z if y is None else y
 
     @staticmethod
     @once_differentiable
@@ -211,9 +210,9 @@ class _Join(torch.autograd.Function):
         if all(t is None for t in douts):
             return (None,) * (2 + len(laid))
         with _device(x):
-            douts = [None if t is None else _dense(t, x.shape[1]) for t in douts]
             dy = douts[0] if laid[1] is not None else None
             dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
+            dy, dz = (None if t is None else _aligned(t) for t in (dy, dz))
             grads = [torch.empty(s, dtype=x.dtype, device=x.device) if n else None
                      for s, n in zip(ctx.shapes, ctx.needs_input_grad[2:])]
             ws = ctypes.c_size_t()
@@ -225,20 +224,19 @@ class _Join(torch.autograd.Function):
         return (None, None, *grads)
 
 
-def _dense(t: torch.Tensor, dim: int) -> torch.Tensor:
-    m = t.reshape(-1, dim).contiguous()
-    return m if m.data_ptr() % 16 == 0 else m.clone()
+def _aligned(t: torch.Tensor) -> torch.Tensor:
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
 def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
     """The inputs as the library reads them; the row strides go into d."""
-    dim = d.dim
-    out = [None if t is None else t.detach() for t in tensors]
-    out[0], d.ldx = _rows(out[0], dim)
+    out = list(tensors)
+    out[0], d.ldx = _rows(out[0], d.dim)
     if out[1] is not None:
-        out[1], d.ldf = _rows(out[1], dim)
+        out[1], d.ldf = _rows(out[1], d.dim)
     if out[4] is not None:
-        out[4], d.ld_gate = _rows(out[4], dim)
+        out[4], d.ld_gate = _rows(out[4], d.dim)
     return out
 
 
@@ -276,13 +274,11 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
     if kind not in _NORM:
         raise ValueError(f"kind must be one of {list(_NORM)}")
     dim, gate = x.shape[-1], tensors[4]
-    for t, name in zip(tensors, _JOIN):
-        if name in ("x", "gate"):
-            continue
-        if name == "f":
-            _check_like(t, x.shape, x, name)
-        else:
-            _check_vector(t, (dim,), x, name)
+    if f is not None:
+        _check_like(f, x.shape, x, "f")
+    for i in _VECTORS:
+        if tensors[i] is not None:
+            _check_dense(tensors[i], (dim,), x, _JOIN[i])
     rows = x.numel() // dim
     d = _lib.Join(rows, dim, _DTYPE[x.dtype], _NORM[kind], (_lib.JOIN_POST if post else 0) | (_lib.JOIN_PRE if pre else 0),
                   0, 0, 0, 0, float(eps), float(alpha), float(p), int(site))
@@ -291,9 +287,8 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
         d.gate_rows = _gate_rows(gate, x)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         return _Join.apply(d, rng, *tensors)
-    y, z = _join_run(d, _join_layout(d, tensors), rng, f is not None)
-    outs = tuple(t.view(x.shape) for t in (y, z) if t is not None)
-    return outs if len(outs) > 1 else outs[0]
+    y, z = _join_run(d, x.shape, _join_layout(d, tensors), rng)
+    return (y, z) if y is not None and z is not None else z if y is None else y
 
 
 def block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -338,9 +333,7 @@ def block_join(x: torch.Tensor, f: torch.Tensor, *, post: Optional[bool] = None,
 
 def _dropout_run(x: torch.Tensor, p: float, rng, site: int) -> torch.Tensor:
     with _device(x):
-        x = x.contiguous()
-        if x.data_ptr() % 16:
-            x = x.clone()
+        x = _aligned(x)
         y = torch.empty_like(x)
         check(lib().slorr_dropout(x.numel(), _DTYPE[x.dtype], p, _ptr(rng), site, x.data_ptr(), y.data_ptr(), _stream(x)),
               "slorr_dropout")

@@ -20,7 +20,7 @@ constexpr int64_t kMaxWidth = int64_t(1) << 20;      // dim, inner
 constexpr int64_t kMaxStride = (int64_t(1) << 22) - 8;   // row strides, in elements: the 256 rows
                                                      // of a tile stay within 2 GiB
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1024;
-constexpr int kFewTokens = 0;
+constexpr int kFewTokens = 64;                       // forward alone: k_few up to here
 constexpr int kMaxNorm = 8192;                       // dim of a join: 512 threads, two pieces of 8 each
 
 inline int64_t up8(int64_t n) { return (n + 7) & ~int64_t(7); }

@@ -46,6 +46,66 @@ __device__ __forceinline__ u32x4 gload16_stream(const void *p) {
   return __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4 *)p);
 }
 
+// 8 consecutive values as loaded. Rows need no 16-byte alignment: the memory
+// system takes 16-byte accesses at any multiple of the element.
+template <typename T>
+struct Raw {
+  u32x4 q[sizeof(T) / 2];
+};
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
+#define SLORR_GLOBAL __attribute__((address_space(1)))
+
+// The end of a row, n < 8 values, goes as runs of 4, 2 and 1: three accesses with
+// one address between them (a load and a store per value cost these kernels 50
+// registers, and with them half of their waves).
+template <typename T>
+__device__ __forceinline__ Raw<T> get(const T *row, int c, int dim) {
+  Raw<T> r;
+  if (c + 8 <= dim) {
+    const SLORR_GLOBAL u32x4_any *p = (const SLORR_GLOBAL u32x4_any *)(row + c);
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) r.q[i] = p[i];
+    return r;
+  }
+#pragma unroll
+  for (int i = 0; i < int(sizeof(T) / 2); ++i) r.q[i] = u32x4{0, 0, 0, 0};
+  const int n = dim - c;
+  if (n <= 0) return r;
+  const bool h4 = n & 4, h2 = n & 2;
+  const T *p2 = row + c + (n & 4), *p1 = row + c + (n & 6);
+  if constexpr (sizeof(T) == 2) {
+    u32x2_any a{0, 0};
+    uint32_t b = 0, d = 0;
+    if (h4) a = *(const SLORR_GLOBAL u32x2_any *)(row + c);
+    if (h2) b = *(const SLORR_GLOBAL u32_any *)p2;
+    if (n & 1) d = *(const SLORR_GLOBAL uint16_t *)p1;
+    const uint32_t lo = h2 ? b : d, hi = h2 ? d : 0u;
+    r.q[0] = u32x4{h4 ? a[0] : lo, h4 ? a[1] : hi, h4 ? lo : 0u, h4 ? hi : 0u};
+  } else {
+    u32x4 a{0, 0, 0, 0};
+    u32x2_any b{0, 0};
+    uint32_t d = 0;
+    if (h4) a = *(const SLORR_GLOBAL u32x4_any *)(row + c);
+    if (h2) b = *(const SLORR_GLOBAL u32x2_any *)p2;
+    if (n & 1) d = *(const SLORR_GLOBAL u32_any *)p1;
+    const uint32_t e0 = h2 ? b[0] : d, e1 = h2 ? b[1] : 0u, e2 = h2 ? d : 0u;
+    r.q[0] = h4 ? a : u32x4{e0, e1, e2, 0u};
+    if (h4) r.q[sizeof(T) / 2 - 1] = u32x4{e0, e1, e2, 0u};
+  }
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void widen(const Raw<T> &r, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (sizeof(T) == 2) v[j] = __uint_as_float(j & 1 ? r.q[0][j >> 1] & 0xffff0000u : r.q[0][j >> 1] << 16);
+    else v[j] = __uint_as_float(r.q[j >> 2][j & 3]);
+  }
+}
+
 // Byte offset of 16-byte chunk `chunk` of LDS row `row`. The XOR key
 // (row & 7) ^ ((row >> 3) & 1) permutes the chunks so that (a) any 8
 // consecutive rows (one 8-lane phase of a 16-byte read with 32 banks) use 8

@@ -162,11 +162,29 @@ FfnProb product(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_
   return p;
 }
 
+template <bool DUAL, bool F32>
+void launch_few(const FewArgs &a, hipStream_t st) {
+  // waves: at least two chunks of k each
+  const int chunks = int(cdiv(a.k, F32 ? 32 : 64)), most = a.tokens > 32 ? 8 : 16;
+  int waves = 4;
+  while (waves < most && chunks >= 4 * waves) waves *= 2;
+  const dim3 grid(uint32_t(cdiv(a.n, 16))), block(64 * waves);
+  if (a.tokens > 32) hipLaunchKernelGGL((k_few<4, DUAL, F32>), grid, block, 0, st, a);
+  else if (a.tokens > 16) hipLaunchKernelGGL((k_few<2, DUAL, F32>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_few<1, DUAL, F32>), grid, block, 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+}
+
 template <bool F32>
 void forward(const FfnShape &s, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *state,
              char *ws, hipStream_t st) {
   const FfnLayout l = ffn_layout(s, false);
   const int64_t T = s.tokens;
+  if (s.few() && !state) {
+    launch_few<true, F32>({x, wg, wu, ws, s.ldx, s.ldf(), int32_t(T), s.inner, s.dim, s.act}, st);
+    launch_few<false, F32>({ws, wd, nullptr, y, s.ldf(), s.dim, int32_t(T), s.dim, s.inner, s.act}, st);
+    return;
+  }
   Layer<F32> lay{s, ws};
   const Operand X = lay.add(x, T, s.dim, s.ldx, l.x);
   const Operand G = lay.add(wg, s.inner, s.dim, s.dim, l.wg);

@@ -482,4 +482,108 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// The forward products for a few tokens (TF x 16 at most), whose time is the
+// reading of the weights: a block takes 16 rows of each weight (DUAL: of Wg and
+// Wu) and its waves share k in chunks of 128 bytes per row; a lane's 16 bytes of
+// a weight row go from memory to the matrix instruction's operand as they are
+// (lane l: row l % 16, k from 8 (l / 16) on; fp32: four k of 4 (l / 16) on in
+// four instructions), the tokens are the other operand, read through the caches
+// by every block. The waves' sums meet in LDS. No row alignment is needed.
+struct FewArgs {
+  const void *x, *w0, *w1;
+  void *out;                   // h or y
+  int64_t ldx, ldo;
+  int32_t tokens, n, k, act;
+};
+
+template <int TF, bool DUAL, bool F32>
+__global__ __launch_bounds__(TF > 2 ? 512 : 1024) void k_few(FewArgs a) {
+  using T = typename std::conditional<F32, float, uint16_t>::type;
+  constexpr int NF = DUAL ? 2 : 1, kWaves = TF > 2 ? 8 : 16;
+  constexpr int kChunk = F32 ? 32 : 64;                // k per chunk of 128 bytes
+  constexpr int kLane = F32 ? 4 : 8, kStep = 4 * kLane;
+  __shared__ float4v red[kWaves][NF * TF][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = int(blockDim.x) >> 6;
+  const int n0 = int(blockIdx.x) * 16, r = lane & 15, kl = (lane >> 4) * kLane;
+  // rows past the end read the last one again; their results go nowhere
+  const int64_t wrow = int64_t(min(n0 + r, a.n - 1)) * a.k;
+  const T *w[NF], *x[TF];
+  w[0] = static_cast<const T *>(a.w0) + wrow;
+  if constexpr (DUAL) w[NF - 1] = static_cast<const T *>(a.w1) + wrow;
+#pragma unroll
+  for (int t = 0; t < TF; ++t) x[t] = static_cast<const T *>(a.x) + int64_t(min(16 * t + r, a.tokens - 1)) * a.ldx;
+  float4v acc[NF][TF];
+#pragma unroll
+  for (int i = 0; i < NF; ++i)
+#pragma unroll
+    for (int t = 0; t < TF; ++t) acc[i][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+  auto load = [&](const T *row, int k) {
+    if constexpr (F32) {
+      if (k + 4 <= a.k) return *(const SLORR_GLOBAL u32x4_any *)(row + k);
+      u32x4_any v{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (k + j < a.k) v[j] = __float_as_uint(row[k + j]);
+      return v;
+    } else {
+      return get(row, k, a.k).q[0];
+    }
+  };
+  for (int k0 = wave * kChunk; k0 < a.k; k0 += waves * kChunk) {
+    u32x4 fw[2][NF], fx[2][TF];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int i = 0; i < NF; ++i) fw[s][i] = load(w[i], k0 + s * kStep + kl);
+#pragma unroll
+      for (int t = 0; t < TF; ++t) fx[s][t] = load(x[t], k0 + s * kStep + kl);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int t = 0; t < TF; ++t) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fw[s][i][j]), __uint_as_float(fx[s][t][j]),
+                                                               acc[i][t], 0, 0, 0);
+          } else {
+            acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[s][i]),
+                                                                __builtin_bit_cast(bf16x8, fx[s][t]), acc[i][t], 0, 0, 0);
+          }
+        }
+  }
+#pragma unroll
+  for (int i = 0; i < NF; ++i)
+#pragma unroll
+    for (int t = 0; t < TF; ++t) red[wave][i * TF + t][lane] = acc[i][t];
+  __syncthreads();
+  // lane l of result block t: token 16 t + l % 16, rows 4 (l / 16) .. + 3
+  for (int t = wave; t < TF; t += waves) {
+    float4v s[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      s[i] = red[0][i * TF + t][lane];
+      for (int q = 1; q < waves; ++q) s[i] += red[q][i * TF + t][lane];
+    }
+    const int token = 16 * t + r, n = n0 + 4 * (lane >> 4);
+    if (token >= a.tokens) continue;
+    T *o = static_cast<T *>(a.out) + token * a.ldo + n;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v = s[0][j];
+      if constexpr (DUAL) {
+        float f, slope;
+        act_and_slope<F32>(a.act, v, f, slope);
+        v = f * s[NF - 1][j];
+      }
+      if (n + j < a.n) o[j] = from_f<T>(v);
+    }
+  }
+}
+
 }  // namespace slorr
