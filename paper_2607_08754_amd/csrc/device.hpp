@@ -128,6 +128,14 @@ __device__ __forceinline__ int swz(int row, int chunk) { return row * 128 + ((ch
 // that those read the other stage). Completion is the caller's job: each
 // k-slab is waited for by count (s_waitcnt vmcnt) before the block barrier
 // that publishes it.
+//
+// The compiler does not see a memory instruction in the assembly either, and so
+// keeps none of the distances that one needs: one wait state after m0 was
+// written, and five after a vector instruction wrote one of its scalar registers.
+// WAIT + 1 of them stand here: 0 where the operands come from scalar
+// instructions, 4 where v_readfirstlane may have written them. Kernels with more
+// scalar values than registers, where v_readlane can come right before a fetch,
+// use fetch_run below.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ i32x4 buffer_rsrc(const void *base, uint32_t bytes) {
   const uint64_t b = uint64_t(uintptr_t(base));
@@ -138,11 +146,12 @@ __device__ __forceinline__ i32x4 buffer_rsrc(const void *base, uint32_t bytes) {
   r[3] = 0x00020000;                                                         // raw 32-bit dwords
   return r;
 }
+template <int WAIT = 0>
 __device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds_base) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const uint32_t m = __builtin_amdgcn_readfirstlane(lds_base);
   const uint32_t so = __builtin_amdgcn_readfirstlane(soff);
-  asm volatile("buffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(m), "v"(voff), "s"(rsrc), "s"(so) : "memory");
+  asm volatile("s_nop %4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(m), "v"(voff), "s"(rsrc), "s"(so), "n"(WAIT) : "memory");
 #else
   (void)rsrc;
   (void)voff;
@@ -152,6 +161,41 @@ __device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uin
 }
 __device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uint32_t soff, void *lds_base) {
   buffer_load_lds16(rsrc, voff, soff, uint32_t(uintptr_t(lds_base)));
+}
+
+// N fetches in a row (see buffer_load_lds16): fetch i takes byte voff + i soff_step
+// of the buffer to lds_base + i kLdsStep + 16 l. One block of assembly, which keeps
+// its own distances: five wait states ahead of the first fetch for the operands'
+// sake (without them fetches took an operand's old value where the compiler's
+// v_readlane came right before: an fp32 product of 4 x 64 x 64 was off by 3e-6 now
+// and then), and one between each write of m0 and its fetch.
+template <int N, int kLdsStep>
+__device__ __forceinline__ void fetch_run(i32x4 rsrc, uint32_t voff, uint32_t soff_step, uint32_t lds_base) {
+  static_assert(N == 2 || N == 4 || N == 8, "fetches in a row");
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t m = __builtin_amdgcn_readfirstlane(lds_base);
+  const uint32_t step = __builtin_amdgcn_readfirstlane(soff_step);
+  uint32_t so = 0;
+#define SLORR_FETCH "buffer_load_dwordx4 %1, %2, %0 offen lds\n\t"
+#define SLORR_NEXT "s_add_u32 m0, m0, %5\n\ts_add_u32 %0, %0, %4\n\t" SLORR_FETCH
+#define SLORR_FIRST "s_mov_b32 m0, %3\n\ts_nop 4\n\t" SLORR_FETCH
+  if constexpr (N == 2)
+    asm volatile(SLORR_FIRST SLORR_NEXT : "+&s"(so) : "v"(voff), "s"(rsrc), "s"(m), "s"(step), "n"(kLdsStep) : "memory", "m0", "scc");
+  else if constexpr (N == 4)
+    asm volatile(SLORR_FIRST SLORR_NEXT SLORR_NEXT SLORR_NEXT
+                 : "+&s"(so) : "v"(voff), "s"(rsrc), "s"(m), "s"(step), "n"(kLdsStep) : "memory", "m0", "scc");
+  else
+    asm volatile(SLORR_FIRST SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT
+                 : "+&s"(so) : "v"(voff), "s"(rsrc), "s"(m), "s"(step), "n"(kLdsStep) : "memory", "m0", "scc");
+#undef SLORR_FETCH
+#undef SLORR_NEXT
+#undef SLORR_FIRST
+#else
+  (void)rsrc;
+  (void)voff;
+  (void)soff_step;
+  (void)lds_base;
+#endif
 }
 
 // Transposing LDS read of 16-bit values (ds_read_b64_tr_b16). Within each

@@ -4,7 +4,8 @@
 //               their epilogues
 //   k_planes    operands laid out in 16-byte rows: bf16 rows padded to a
 //               multiple of 8, fp32 values as three bf16 planes
-//   k_split_sum a product's partials added in order
+//   k_tail      the parts of tiles that were cut along k, added in order
+//   k_few       the forward products for a few tokens
 #include <algorithm>
 #include <type_traits>
 
@@ -64,43 +65,105 @@ __global__ __launch_bounds__(256) void k_planes(LayArgs args) {
   }
 }
 
-template <bool F32>
-__global__ __launch_bounds__(256) void k_split_sum(FfnProb p) {
-  const int pieces = int(p.ldp >> 3);
-  const int64_t total = int64_t(p.m) * pieces, step = int64_t(p.m) * p.ldp;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-    const int64_t r = i / pieces;
-    const int c = int(i - r * pieces) * 8;
-    float v[8] = {};
-    for (int s = 0; s < p.splits; ++s) {
-      float w[8];
-      load_whole<true>(p.part + s * step, r * p.ldp + c, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += w[j];
-    }
-    if (c < p.n) store_some<F32>(p.out, r * p.ldo + c, p.n - c, v);
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// How a launch's products are cut: tiles of 256 or 128, and how many of them whole.
+struct Cut {
+  int tile = 0;
+  int64_t tiles = 0, whole = 0, cuts = 0, run = 0;
+  int64_t part_bytes() const { return cuts ? (cuts + (tiles - whole)) * tile * tile * 4 : 0; }
+};
+
+// Microseconds per slab of a round of tiles with every CU at work (1536 x 6144,
+// 16384 tokens, bf16: one 256-tile per CU, or two 128-tiles), and with one
+// 128-tile per CU at most, where a slab's latency is all there is.
+constexpr double kSlab256 = 1.75, kSlab128 = 1.35, kSlabAlone = 0.8;
+
+Cut cut_with(int tile, int64_t tiles, int64_t slabs) {
+  Cut c;
+  c.tile = tile;
+  c.tiles = tiles;
+  const int64_t slots = tile == kBigTile ? kCus : 2 * kCus;
+  c.whole = tiles / slots * slots;
+  const int64_t tail = tiles - c.whole, total = tail * slabs;
+  if (!tail) return c;
+  // runs of at least 6 slabs: below, a block's start and its part's way through
+  // memory cost more than the slabs
+  c.run = std::max<int64_t>(6, cdiv(total, slots));
+  if (c.run >= slabs) {
+    c.run = 0;
+    c.whole = tiles;
+    return c;
   }
+  c.cuts = cdiv(total, c.run);
+  return c;
 }
 
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Estimated microseconds: rounds of whole tiles, then the runs with their parts
+// written and read once (4 TB/s) and the launch that adds them.
+double cut_time(const Cut &c, int64_t slabs) {
+  const int64_t slots = c.tile == kBigTile ? kCus : 2 * kCus;
+  auto slab = [&](int64_t blocks) { return c.tile == kBigTile ? kSlab256 : blocks > kCus ? kSlab128 : kSlabAlone; };
+  double t = double(c.whole / slots) * double(slabs) * slab(slots);
+  const int64_t rest = c.whole % slots;
+  if (rest) t += double(slabs) * slab(rest);
+  if (c.cuts) t += double(c.run) * slab(c.cuts) + 5.0 + double(c.part_bytes()) * 2 / 4e6;
+  return t;
+}
+
+template <int EPI, bool F32>
+Cut cut_products(const FfnProb *p, int nprob, int64_t ldf) {
+  Cut best;
+  double least = 0;
+  const int64_t slabs = cdiv(p[0].k, 64) * p[0].nsrc * (F32 ? 6 : 1);
+  for (int tile : {kBigTile, kTile}) {
+    int64_t tiles = 0;
+    for (int i = 0; i < nprob; ++i)
+      tiles += cdiv(p[i].m, tile) * cdiv(EPI == kStore ? p[i].n : ldf, EPI == kAct ? tile / 2 : tile);
+    Cut c = cut_with(tile, tiles, slabs), d = c;          // the tail in runs, or all whole
+    d.whole = tiles;
+    d.cuts = d.run = 0;
+    for (const Cut &x : {c, d}) {
+      const double t = cut_time(x, slabs);
+      if (!best.tile || t < least) {
+        best = x;
+        least = t;
+      }
+    }
+  }
+  return best;
+}
+
+template <int B, int WGM, int WGN, bool AK, bool BK, int EPI, bool F32>
+void launch_tiles(const FfnArgs &a, hipStream_t st) {
+  const dim3 grid(uint32_t(a.whole + a.cuts));
+  hipLaunchKernelGGL((k_ffn<B, B, WGM, WGN, 2, AK, BK, EPI, F32>), grid, dim3(64 * WGM * WGN), 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+  if (!a.cuts) return;
+  const dim3 pieces(uint32_t(B * B / (EPI == kAct ? 16 : 8) / 256), uint32_t(a.tail));
+  hipLaunchKernelGGL((k_tail<B, B, EPI, F32>), pieces, dim3(256), 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+}
 
 template <bool AK, bool BK, int EPI, bool F32>
 void launch_products(FfnArgs &a, hipStream_t st) {
-  constexpr int B = kTile;
-  int64_t units = 0;
+  const Cut c = cut_products<EPI, F32>(a.p, a.nprob, a.ldf);
+  int64_t tiles = 0;
   for (int i = 0; i < a.nprob; ++i) {
     FfnProb &p = a.p[i];
-    p.tm = int32_t(cdiv(p.m, B));
-    p.tn = int32_t(cdiv(EPI == kStore ? p.n : a.ldf, EPI == kAct ? B / 2 : B));
-    p.splits = 1;
-    p.per = int32_t(cdiv(p.k, 64)) * p.nsrc * (F32 ? 6 : 1);
-    p.unit0 = int32_t(units);
-    units += int64_t(p.tm) * p.tn * p.splits;
+    p.tm = int32_t(cdiv(p.m, c.tile));
+    p.tn = int32_t(cdiv(EPI == kStore ? p.n : a.ldf, EPI == kAct ? c.tile / 2 : c.tile));
+    p.tile0 = int32_t(tiles);
+    tiles += int64_t(p.tm) * p.tn;
   }
-  a.units = int32_t(units);
-  if (!units) return;
-  hipLaunchKernelGGL((k_ffn<B, B, 2, 2, 2, AK, BK, EPI, F32>), dim3(uint32_t(units)), dim3(256), 0, st, a);
-  check(hipGetLastError(), "kernel launch");
+  if (!tiles) return;
+  a.whole = int32_t(c.whole);
+  a.tail = int32_t(c.cuts ? tiles - c.whole : 0);
+  a.slabs = int32_t(cdiv(a.p[0].k, 64)) * a.p[0].nsrc * (F32 ? 6 : 1);
+  a.run = int32_t(c.run);
+  a.cuts = int32_t(c.cuts);
+  if (c.tile == kBigTile) launch_tiles<kBigTile, 2, 4, AK, BK, EPI, F32>(a, st);
+  else launch_tiles<kTile, 2, 2, AK, BK, EPI, F32>(a, st);
 }
 
 // The state's parts: a, b, and in bf16 a byte per 8 values of each.
@@ -196,6 +259,7 @@ void forward(const FfnShape &s, const void *x, const void *wg, const void *wu, c
   a.nprob = 1;
   a.act = s.act;
   a.ldf = int32_t(s.ldf());
+  a.part = reinterpret_cast<float *>(ws + l.part);
   a.p[0] = product(X, G, T, s.inner, s.dim, nullptr, 0);
   a.p[0].b[1] = U.p;
   state_parts(s, state, a);
@@ -227,6 +291,7 @@ void backward(const FfnShape &s, const void *dy, const void *x, const void *wg, 
   FfnArgs a{};
   a.act = s.act;
   a.ldf = int32_t(s.ldf());
+  a.part = reinterpret_cast<float *>(ws + l.part);
   if (T) {
     a.nprob = 1;
     a.p[0] = product(DY, D, T, s.inner, s.dim, nullptr, 0);
@@ -277,6 +342,33 @@ FfnLayout ffn_layout(const FfnShape &s, bool bwd) {
     l.da = take(T * size_t(s.ldf()) * pl);
     l.db = take(T * size_t(s.ldf()) * pl);
   }
+  // parts of cut tiles: what the launches of the call need at most (the weight
+  // gradients that are asked for are a launch of one to three products)
+  const bool f32 = s.dtype == SLORR_F32;
+  auto need = [&](auto epi, int nprob, int64_t m, int64_t n, int64_t k, int nsrc) {
+    constexpr int EPI = decltype(epi)::value;
+    FfnProb p[3]{};
+    for (int i = 0; i < nprob; ++i) {
+      // (dw_down's m and n change places: with square tiles the number is the same)
+      p[i].m = int32_t(m);
+      p[i].n = int32_t(n);
+      p[i].k = int32_t(k);
+      p[i].nsrc = nsrc;
+    }
+    const Cut c = f32 ? cut_products<EPI, true>(p, nprob, s.ldf()) : cut_products<EPI, false>(p, nprob, s.ldf());
+    return size_t(c.part_bytes());
+  };
+  std::integral_constant<int, kStore> store;
+  size_t part = 0;
+  if (!bwd) {
+    part = std::max(need(std::integral_constant<int, kAct>{}, 1, s.tokens, s.inner, s.dim, 1),
+                    need(store, 1, s.tokens, s.dim, s.inner, 1));
+  } else {
+    part = std::max(need(std::integral_constant<int, kActBack>{}, 1, s.tokens, s.inner, s.dim, 1),
+                    need(store, 1, s.tokens, s.dim, s.inner, 2));
+    for (int i = 1; i <= 3; ++i) part = std::max(part, need(store, i, s.inner, s.dim, s.tokens, 1));
+  }
+  l.part = take(part);
   l.bytes = std::max(l.bytes, size_t(256));
   return l;
 }

@@ -35,17 +35,22 @@ struct FfnProb {               // one product C (m x n) = sum over sources of A 
   int64_t lda, ldb;            // elements per row
   int32_t m, n, k, nsrc;
   int32_t tm, tn;              // tiles
-  int32_t splits, per;         // parts of the k range, slabs per part
-  int32_t unit0;               // the first block of this product in the launch
+  int32_t tile0;               // the first tile of this product in the launch
   void *out;
   int64_t ldo;
-  float *part;                 // splits > 1: fp32 partials [split][m][ldp]
-  int64_t ldp;
 };
 
+// A launch's tiles (those of all its products, with `slabs` slabs of k each): the
+// first `whole` are a block's each. The slabs of the `tail` others are laid end
+// to end and cut into `cuts` runs of `run`, a block's each: a launch ends with
+// all CUs at work, however few tiles it has. A block that holds a part of a tile
+// stores its fp32 sums; block c and tail tile t share slot c + t (along the
+// runs one of the two grows at a time), and k_tail adds a tile's slots in order.
 struct FfnArgs {
   FfnProb p[3];
-  int32_t nprob, units, act;
+  int32_t nprob, act;
+  int32_t whole, tail, slabs, run, cuts;
+  float *part;
   int32_t ldf;                 // row length of the inner tensors
   void *sa, *sb;               // a, b as kept for the backward pass (kAct: may be null)
   uint8_t *ea, *eb;            // their exponents (bf16 tensors)
@@ -257,6 +262,58 @@ __device__ __forceinline__ int plane_pair(int i) {
   return int((t >> (4 * i)) & 15u);
 }
 
+// The corner of a product's tile t: 8 tiles of a column of tiles follow each other.
+template <int BM, int BN, int EPI>
+__device__ __forceinline__ void tile_corner(const FfnProb &p, int t, int &m0, int &n0) {
+  const int gsize = 8 * p.tn, g = t / gsize, r = t - g * gsize;
+  const int rows = min(8, p.tm - 8 * g), c = r / rows;
+  m0 = (8 * g + r - c * rows) * BM;
+  n0 = c * (EPI == kAct ? BN / 2 : BN);
+}
+
+// What becomes of 8 consecutive sums v of row `row` from column `col` on; kAct: of
+// a's (v) and b's.
+template <int EPI, bool F32>
+__device__ __forceinline__ void finish(const FfnArgs &args, const FfnProb &pr, int row, int col, float (&v)[8],
+                                       float (&b)[8]) {
+  if (row >= pr.m) return;
+  if constexpr (EPI == kStore) {
+    if (col < pr.n) store_some<F32>(pr.out, int64_t(row) * pr.ldo + col, pr.n - col, v);
+    return;
+  }
+  if (col >= args.ldf) return;
+  const int64_t at = int64_t(row) * args.ldf + col;
+  float h[8];
+  if constexpr (EPI == kAct) {
+    if (args.sa) {
+      store_kept<F32>(args.sa, args.ea, at, v);
+      store_kept<F32>(args.sb, args.eb, at, b);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float f, sl;
+      act_and_slope<F32>(args.act, v[j], f, sl);
+      h[j] = f * b[j];
+    }
+    store_planes<F32>(args.h + at * 2, args.plane, h);
+  } else {
+    float a[8], da[8], db[8];
+    load_kept<F32>(args.sa, args.ea, at, a);
+    load_kept<F32>(args.sb, args.eb, at, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float f, sl;
+      act_and_slope<F32>(args.act, a[j], f, sl);
+      h[j] = f * b[j];
+      db[j] = v[j] * f;
+      da[j] = v[j] * b[j] * sl;
+    }
+    store_planes<F32>(args.h + at * 2, args.plane, h);
+    store_planes<F32>(args.da + at * 2, args.plane, da);
+    store_planes<F32>(args.db + at * 2, args.plane, db);
+  }
+}
+
 template <int BM, int BN, int WGM, int WGN, int NS, bool AK, bool BK, int EPI, bool F32>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
   using S = FfnTile<BM, BN, WGM, WGN, NS, AK, BK>;
@@ -266,52 +323,60 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
   const int lr = lane & 31, lk = lane >> 5;
   const int wm = wave / WGN, wn = wave % WGN;
 
-  // Block -> unit: each XCD (block index modulo 8) takes a run of consecutive
-  // units, in which 8 tiles of one column of tiles follow each other, so the
-  // blocks of an XCD share operand panels in its L2.
-  int unit;
-  {
-    const int b = int(blockIdx.x), xcd = b & 7, per = args.units >> 3, rem = args.units & 7;
-    unit = xcd * per + min(xcd, rem) + (b >> 3);
-  }
+  // Block -> tile, or run of the tail: each XCD (block index modulo 8; `whole` is
+  // a multiple of 8) takes consecutive ones, in which 8 tiles of one column of
+  // tiles follow each other, so the blocks of an XCD share operand panels in its
+  // L2.
+  auto by_xcd = [](int b, int n) {
+    const int xcd = b & 7, per = n >> 3, rem = n & 7;
+    return xcd * per + min(xcd, rem) + (b >> 3);
+  };
+  const bool in_tail = int(blockIdx.x) >= args.whole;
+  const int cut = in_tail ? by_xcd(int(blockIdx.x) - args.whole, args.cuts) : 0;
+  int64_t pos = in_tail ? int64_t(cut) * args.run : int64_t(by_xcd(int(blockIdx.x), args.whole)) * args.slabs;
+  const int64_t end = in_tail ? min(pos + args.run, int64_t(args.tail) * args.slabs) : pos + args.slabs;
+  // (a block of no slabs, k = 0, stores its tile's zeros)
+  for (bool once = true; once || pos < end; once = false) {
+  const int tt = args.slabs ? int(pos / args.slabs) : in_tail ? cut : by_xcd(int(blockIdx.x), args.whole);
+  const int s0 = int(pos - int64_t(tt) * args.slabs), s1 = int(min(int64_t(args.slabs), s0 + end - pos)), ns = s1 - s0;
+  pos += ns;
+  const int tile = in_tail ? args.whole + tt : tt;
   FfnProb pr = args.p[0];
-  if (args.nprob > 1 && unit >= args.p[1].unit0) pr = args.p[1];
-  if (args.nprob > 2 && unit >= args.p[2].unit0) pr = args.p[2];
-  unit -= pr.unit0;
-  const int tiles = pr.tm * pr.tn;
-  const int split = unit / tiles;
+  if (args.nprob > 1 && tile >= args.p[1].tile0) pr = args.p[1];
+  if (args.nprob > 2 && tile >= args.p[2].tile0) pr = args.p[2];
   int m0, n0;
-  {
-    const int t = unit - split * tiles, gsize = 8 * pr.tn, g = t / gsize, r = t - g * gsize;
-    const int rows = min(8, pr.tm - 8 * g), c = r / rows;
-    m0 = (8 * g + r - c * rows) * BM;
-    n0 = c * (EPI == kAct ? BN / 2 : BN);
-  }
+  tile_corner<BM, BN, EPI>(pr, tile - pr.tile0, m0, n0);
   // k: nsrc (times six passes) segments of nkt slabs; this block's slabs [s0, s1)
   const int nkt = (pr.k + 63) >> 6;
   const int kp = (pr.k + 7) & ~7;
-  const int nseg = (F32 ? 6 : 1) * pr.nsrc;
-  const int s0 = split * pr.per, s1 = min(nseg * nkt, s0 + pr.per), ns = s1 - s0;
   int seg = nkt ? s0 / nkt : 0, kt = s0 - seg * nkt;      // the next slab to fetch
 
   const uint32_t lds0 = lds_offset(smem);
   auto clamp31 = [](int64_t v) { return uint32_t(v < 0x7fffffff ? v : 0x7fffffff); };
-  // rows: `limit` valid rows from the tile's first on
-  auto fetch_rows = [&](const char *base, int64_t ld, int64_t limit, int k0, uint32_t dst, int i, int row_step) {
+  // N fetches of 8 rows each, row_step rows apart, to every FW-th (twice: 2 FW-th)
+  // KB of the stage from `dst` on; `limit` valid rows from the first on
+  auto fetch_rows = [&](auto n, auto lds_step, const char *base, int64_t ld, int64_t limit, int k0, uint32_t dst,
+                        int row_step) {
     const i32x4 rs = buffer_rsrc(base + int64_t(k0) * 2, limit > 0 ? clamp31(((limit - 1) * ld + kp - k0) * 2) : 0u);
     const int row = wave * 8 + (lane >> 3), c = (lane & 7) ^ swz_key(row);
     uint32_t voff = (uint32_t(row) * uint32_t(ld) + uint32_t(c * 8)) * 2u;
     if (k0 + 64 > kp && k0 + c * 8 >= kp) voff = 0x80000000u;
-    buffer_load_lds16(rs, voff, uint32_t(row_step) * uint32_t(ld) * 2u, dst + (wave + i * FW) * 1024);
+    fetch_run<decltype(n)::value, decltype(lds_step)::value>(rs, voff, uint32_t(row_step) * uint32_t(ld) * 2u, dst + wave * 1024);
   };
-  auto fetch_kn = [&](const char *base, int64_t ld, int pitch, int k0, int cols, uint32_t dst, int loads) {
+  auto fetch_kn = [&](auto n, auto pitch_c, const char *base, int64_t ld, int k0, int cols, uint32_t dst) {
+    constexpr int pitch = decltype(pitch_c)::value, cpr = pitch / 16, rpx = 1024 / pitch;
     const i32x4 rs = buffer_rsrc(base + int64_t(k0) * ld * 2, clamp31((int64_t(pr.k - k0 - 1) * ld + cols) * 2));
-    const int cpr = pitch / 16, rpx = 1024 / pitch;
     const int row = wave * rpx + lane / cpr;
     const uint32_t voff = (uint32_t(row) * uint32_t(ld) + uint32_t(((lane % cpr) ^ ((row & 3) << 2)) * 8)) * 2u;
-    for (int i = 0; i < loads; ++i)
-      buffer_load_lds16(rs, voff, uint32_t(i * rpx * FW) * uint32_t(ld) * 2u, dst + (wave + i * FW) * 1024);
+    fetch_run<decltype(n)::value, FW * 1024>(rs, voff, uint32_t(rpx * FW) * uint32_t(ld) * 2u, dst + wave * 1024);
   };
+  constexpr std::integral_constant<int, S::kLoadsA> nA{};
+  constexpr std::integral_constant<int, S::kLoadsB> nB{};
+  constexpr std::integral_constant<int, S::kLoadsB / 2> nHalf{};
+  constexpr std::integral_constant<int, FW * 1024> each{};
+  constexpr std::integral_constant<int, 2 * FW * 1024> other{};
+  constexpr std::integral_constant<int, BM * 2> pitchA{};
+  constexpr std::integral_constant<int, BN * 2> pitchB{};
   auto dload = [&](int st) {
     const int src = pr.nsrc > 1 ? seg & 1 : 0;
     int64_t oa = 0, ob = 0;
@@ -332,26 +397,17 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
       A = pr.a[1] + oa;
       B = pr.b[1] + ob;
     }
-    if constexpr (AK) {
-      fetch_kn(A + int64_t(m0) * 2, pr.lda, BM * 2, k0, ((pr.m + 7) & ~7) - m0, sA, S::kLoadsA);
-    } else {
-#pragma unroll
-      for (int i = 0; i < S::kLoadsA; ++i)
-        fetch_rows(A + int64_t(m0) * pr.lda * 2, pr.lda, pr.m - m0, k0, sA, i, i * 8 * FW);
-    }
+    if constexpr (AK) fetch_kn(nA, pitchA, A + int64_t(m0) * 2, pr.lda, k0, ((pr.m + 7) & ~7) - m0, sA);
+    else fetch_rows(nA, each, A + int64_t(m0) * pr.lda * 2, pr.lda, pr.m - m0, k0, sA, 8 * FW);
     if constexpr (BK) {
-      fetch_kn(B + int64_t(n0) * 2, pr.ldb, BN * 2, k0, ((pr.n + 7) & ~7) - n0, sB, S::kLoadsB);
+      fetch_kn(nB, pitchB, B + int64_t(n0) * 2, pr.ldb, k0, ((pr.n + 7) & ~7) - n0, sB);
     } else if constexpr (EPI == kAct) {
       // rows 64 w .. 64 w + 31 of the stage: Wg's rows n0 + 32 w .., the next 32: Wu's
       static_assert(FW == 4, "32 rows per half");
-      const char *U = pr.b[1] + ob;
-#pragma unroll
-      for (int i = 0; i < S::kLoadsB; ++i)
-        fetch_rows(((i & 1) ? U : B) + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB, i, (i >> 1) * 32);
+      fetch_rows(nHalf, other, B + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB, 32);
+      fetch_rows(nHalf, other, pr.b[1] + ob + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB + FW * 1024, 32);
     } else {
-#pragma unroll
-      for (int i = 0; i < S::kLoadsB; ++i)
-        fetch_rows(B + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB, i, i * 8 * FW);
+      fetch_rows(nB, each, B + int64_t(n0) * pr.ldb * 2, pr.ldb, pr.n - n0, k0, sB, 8 * FW);
     }
   };
 
@@ -417,15 +473,15 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
         *reinterpret_cast<float4v *>(ef + lr * S::kPitch + 32 * j + 8 * g + 4 * lk) =
             float4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
     __builtin_amdgcn_wave_barrier();
-    const int row0 = m0 + wm * S::WTM + i * 32;
+    const int row0 = wm * S::WTM + i * 32;
+    const bool part = ns < args.slabs;
     constexpr int PC = EPI == kAct ? 4 : 8;               // 8-column pieces per row
     constexpr int kTasks = 32 * PC / 64;
     constexpr int kCopies = F32 && EPI != kStore ? 1 : kTasks;   // fp32 activations are long code
 #pragma unroll kCopies
     for (int t = 0; t < kTasks; ++t) {
       const int task = lane + 64 * t, rl = task / PC, cl = (task % PC) * 8;
-      const int row = row0 + rl;
-      float v[8];
+      float v[8], b[8];
       auto staged = [&](int c, float (&o)[8]) {
         const float4v e0 = *reinterpret_cast<const float4v *>(ef + rl * S::kPitch + c);
         const float4v e1 = *reinterpret_cast<const float4v *>(ef + rl * S::kPitch + c + 4);
@@ -433,53 +489,52 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
         for (int j = 0; j < 8; ++j) o[j] = j < 4 ? e0[j & 3] : e1[j & 3];
       };
       staged(cl, v);
-      if constexpr (EPI == kAct) {
-        const int col = n0 + wn * 32 + cl;
-        float b[8], h[8];
-        staged(32 + cl, b);
-        if (row < pr.m && col < args.ldf) {
-          const int64_t at = int64_t(row) * args.ldf + col;
-          if (args.sa) {
-            store_kept<F32>(args.sa, args.ea, at, v);
-            store_kept<F32>(args.sb, args.eb, at, b);
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float f, sl;
-            act_and_slope<F32>(args.act, v[j], f, sl);
-            h[j] = f * b[j];
-          }
-          store_planes<F32>(args.h + at * 2, args.plane, h);
-        }
-      } else if constexpr (EPI == kActBack) {
-        const int col = n0 + wn * 64 + cl;
-        if (row < pr.m && col < args.ldf) {
-          const int64_t at = int64_t(row) * args.ldf + col;
-          float a[8], b[8], h[8], da[8], db[8];
-          load_kept<F32>(args.sa, args.ea, at, a);
-          load_kept<F32>(args.sb, args.eb, at, b);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float f, sl;
-            act_and_slope<F32>(args.act, a[j], f, sl);
-            h[j] = f * b[j];
-            db[j] = v[j] * f;
-            da[j] = v[j] * b[j] * sl;
-          }
-          store_planes<F32>(args.h + at * 2, args.plane, h);
-          store_planes<F32>(args.da + at * 2, args.plane, da);
-          store_planes<F32>(args.db + at * 2, args.plane, db);
-        }
+      if constexpr (EPI == kAct) staged(32 + cl, b);
+      if (part) {
+        const int64_t at = (int64_t(cut + tt) * BM + row0 + rl) * BN + wn * 64 + cl;
+        store_whole<true>(args.part, at, v);
+        if constexpr (EPI == kAct) store_whole<true>(args.part, at + 32, b);
       } else {
-        const int col = n0 + wn * 64 + cl;
-        if (row < pr.m && col < pr.n) {
-          if (pr.splits > 1) store_whole<true>(pr.part + (int64_t(split) * pr.m + row) * pr.ldp, col, v);
-          else store_some<F32>(pr.out, int64_t(row) * pr.ldo + col, pr.n - col, v);
-        }
+        finish<EPI, F32>(args, pr, m0 + row0 + rl, n0 + wn * (EPI == kAct ? 32 : 64) + cl, v, b);
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
+  if (pos < end) __syncthreads();    // the next tile's slabs go where the sums were staged
+  }
+}
+
+// The sums of a tail tile's parts, in the order of k, and what becomes of them.
+template <int BM, int BN, int EPI, bool F32>
+__global__ __launch_bounds__(256) void k_tail(FfnArgs args) {
+  constexpr int PC = EPI == kAct ? BN / 16 : BN / 8;      // pieces per tile row
+  const int tt = blockIdx.y, tile = args.whole + tt;
+  const int64_t start = int64_t(tt) * args.slabs, last = start + args.slabs - 1;
+  const int c0 = int(start / args.run), c1 = int(last / args.run);
+  if (c0 == c1) return;                                   // one block had the whole tile
+  FfnProb pr = args.p[0];
+  if (args.nprob > 1 && tile >= args.p[1].tile0) pr = args.p[1];
+  if (args.nprob > 2 && tile >= args.p[2].tile0) pr = args.p[2];
+  int m0, n0;
+  tile_corner<BM, BN, EPI>(pr, tile - pr.tile0, m0, n0);
+  const int task = int(blockIdx.x) * 256 + threadIdx.x, row = task / PC, q = task % PC;
+  if (row >= BM || m0 + row >= pr.m) return;
+  // kAct: piece q is columns 8 q of h; its a and b sums lie 32 columns apart
+  const int col = EPI == kAct ? (q >> 2) * 64 + (q & 3) * 8 : q * 8;
+  float v[8] = {}, b[8] = {};
+  for (int c = c0; c <= c1; ++c) {
+    const int64_t at = (int64_t(c + tt) * BM + row) * BN + col;
+    float w[8];
+    load_whole<true>(args.part, at, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += w[j];
+    if constexpr (EPI == kAct) {
+      load_whole<true>(args.part, at + 32, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] += w[j];
+    }
+  }
+  finish<EPI, F32>(args, pr, m0 + row, n0 + q * 8, v, b);
 }
 
 // ---------------------------------------------------------------------------

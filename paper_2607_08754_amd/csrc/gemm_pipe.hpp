@@ -273,9 +273,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_tile(GemmArgs args) {
       const uint32_t voff = (uint32_t(row) * uint32_t(ldb) +
                              uint32_t(n0 + ((lane % CPR) ^ ((row & 3) << 2)) * V)) * uint32_t(sizeof(T));
 #pragma unroll
-      for (int i = 0; i < S::kLoadsB; ++i)
-        buffer_load_lds16(rb, voff, (uint32_t(k0) + uint32_t(i * S::RPX * S::kFW)) * uint32_t(ldb) * uint32_t(sizeof(T)),
-                          sB + (wave + i * S::kFW) * 1024);
+      for (int i = 0; i < S::kLoadsB; ++i)      // (the row pitch comes from a vector register)
+        buffer_load_lds16<4>(rb, voff, (uint32_t(k0) + uint32_t(i * S::RPX * S::kFW)) * uint32_t(ldb) * uint32_t(sizeof(T)),
+                             sB + (wave + i * S::kFW) * 1024);
     } else if (!diag) {
       fetch_rows(Bp, bbytes, ldb, n0, k0, sB);
     }
