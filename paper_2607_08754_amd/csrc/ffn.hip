@@ -67,68 +67,57 @@ __global__ __launch_bounds__(256) void k_planes(LayArgs args) {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a launch's products are cut: tiles of 256 or 128, and how many of them whole.
+// How a launch's products are cut: tiles of 256 or 128, how many of them whole,
+// and the parts of the others.
 struct Cut {
   int tile = 0;
-  int64_t tiles = 0, whole = 0, cuts = 0, run = 0;
-  int64_t part_bytes() const { return cuts ? (cuts + (tiles - whole)) * tile * tile * 4 : 0; }
+  int64_t whole = 0, tail = 0, parts = 0, per = 0;
+  size_t part_bytes() const { return size_t(tail * parts) * size_t(tile) * size_t(tile) * 4; }
 };
 
 // Microseconds per slab of a round of tiles with every CU at work (1536 x 6144,
 // 16384 tokens, bf16: one 256-tile per CU, or two 128-tiles), and with one
-// 128-tile per CU at most, where a slab's latency is all there is.
-constexpr double kSlab256 = 1.75, kSlab128 = 1.35, kSlabAlone = 0.8;
+// 128-tile per CU at most, where a slab's latency is all there is; and per byte
+// of the parts, written and read once (4.5 TB/s).
+constexpr double kSlab256 = 1.75, kSlab128 = 1.35, kSlabAlone = 0.8, kPartByte = 2 / 4.5e6;
 
-Cut cut_with(int tile, int64_t tiles, int64_t slabs) {
-  Cut c;
-  c.tile = tile;
-  c.tiles = tiles;
-  const int64_t slots = tile == kBigTile ? kCus : 2 * kCus;
-  c.whole = tiles / slots * slots;
-  const int64_t tail = tiles - c.whole, total = tail * slabs;
-  if (!tail) return c;
-  // runs of at least 6 slabs: below, a block's start and its part's way through
-  // memory cost more than the slabs
-  c.run = std::max<int64_t>(6, cdiv(total, slots));
-  if (c.run >= slabs) {
-    c.run = 0;
-    c.whole = tiles;
-    return c;
-  }
-  c.cuts = cdiv(total, c.run);
-  return c;
-}
-
-// Estimated microseconds: rounds of whole tiles, then the runs with their parts
-// written and read once (4 TB/s) and the launch that adds them.
-double cut_time(const Cut &c, int64_t slabs) {
-  const int64_t slots = c.tile == kBigTile ? kCus : 2 * kCus;
-  auto slab = [&](int64_t blocks) { return c.tile == kBigTile ? kSlab256 : blocks > kCus ? kSlab128 : kSlabAlone; };
-  double t = double(c.whole / slots) * double(slabs) * slab(slots);
-  const int64_t rest = c.whole % slots;
-  if (rest) t += double(slabs) * slab(rest);
-  if (c.cuts) t += double(c.run) * slab(c.cuts) + 5.0 + double(c.part_bytes()) * 2 / 4e6;
-  return t;
-}
-
+// The least of: rounds of whole tiles; whole tiles as long as they fill rounds,
+// the rest cut into parts. 16384 x 1536 x 6144, one 256-tile per CU: y's 384
+// tiles of 96 slabs, two rounds whole 428 us, the last 128 in two parts each 348
+// + 17 us; dx (192 slabs) 701 and 560 + 17. 501 x 1280 x 3456, forward: 68 and 45 us.
 template <int EPI, bool F32>
 Cut cut_products(const FfnProb *p, int nprob, int64_t ldf) {
   Cut best;
   double least = 0;
   const int64_t slabs = cdiv(p[0].k, 64) * p[0].nsrc * (F32 ? 6 : 1);
   for (int tile : {kBigTile, kTile}) {
+    const int64_t slots = tile == kBigTile ? kCus : 2 * kCus;
+    auto round = [&](int64_t units) { return tile == kBigTile ? kSlab256 : units > kCus ? kSlab128 : kSlabAlone; };
+    auto time = [&](int64_t units, int64_t n) {           // units of n slabs
+      const int64_t full = units / slots, rest = units - full * slots;
+      return double(n) * (double(full) * round(slots) + (rest ? round(rest) : 0.0));
+    };
     int64_t tiles = 0;
     for (int i = 0; i < nprob; ++i)
       tiles += cdiv(p[i].m, tile) * cdiv(EPI == kStore ? p[i].n : ldf, EPI == kAct ? tile / 2 : tile);
-    Cut c = cut_with(tile, tiles, slabs), d = c;          // the tail in runs, or all whole
-    d.whole = tiles;
-    d.cuts = d.run = 0;
-    for (const Cut &x : {c, d}) {
-      const double t = cut_time(x, slabs);
+    auto offer = [&](const Cut &c, double t) {
       if (!best.tile || t < least) {
-        best = x;
+        best = c;
         least = t;
       }
+    };
+    Cut c;
+    c.tile = tile;
+    c.whole = tiles;
+    offer(c, time(tiles, slabs));
+    c.whole = tiles / slots * slots;
+    c.tail = tiles - c.whole;
+    // parts of at least 4 slabs: below, a block's start and its part's way through
+    // memory cost more than the slabs
+    for (c.parts = 2; c.tail && c.parts <= 16 && cdiv(slabs, c.parts) >= 4; ++c.parts) {
+      c.per = cdiv(slabs, c.parts);
+      if (c.per * (c.parts - 1) >= slabs) continue;       // (the last part would be empty)
+      offer(c, time(c.whole, slabs) + time(c.tail * c.parts, c.per) + 5.0 + double(c.part_bytes()) * kPartByte);
     }
   }
   return best;
@@ -136,10 +125,10 @@ Cut cut_products(const FfnProb *p, int nprob, int64_t ldf) {
 
 template <int B, int WGM, int WGN, bool AK, bool BK, int EPI, bool F32>
 void launch_tiles(const FfnArgs &a, hipStream_t st) {
-  const dim3 grid(uint32_t(a.whole + a.cuts));
+  const dim3 grid(uint32_t(a.whole + a.tail * a.parts));
   hipLaunchKernelGGL((k_ffn<B, B, WGM, WGN, 2, AK, BK, EPI, F32>), grid, dim3(64 * WGM * WGN), 0, st, a);
   check(hipGetLastError(), "kernel launch");
-  if (!a.cuts) return;
+  if (!a.tail) return;
   const dim3 pieces(uint32_t(B * B / (EPI == kAct ? 16 : 8) / 256), uint32_t(a.tail));
   hipLaunchKernelGGL((k_tail<B, B, EPI, F32>), pieces, dim3(256), 0, st, a);
   check(hipGetLastError(), "kernel launch");
@@ -158,10 +147,10 @@ void launch_products(FfnArgs &a, hipStream_t st) {
   }
   if (!tiles) return;
   a.whole = int32_t(c.whole);
-  a.tail = int32_t(c.cuts ? tiles - c.whole : 0);
+  a.tail = int32_t(c.tail);
   a.slabs = int32_t(cdiv(a.p[0].k, 64)) * a.p[0].nsrc * (F32 ? 6 : 1);
-  a.run = int32_t(c.run);
-  a.cuts = int32_t(c.cuts);
+  a.parts = int32_t(c.parts);
+  a.per = int32_t(c.per);
   if (c.tile == kBigTile) launch_tiles<kBigTile, 2, 4, AK, BK, EPI, F32>(a, st);
   else launch_tiles<kTile, 2, 2, AK, BK, EPI, F32>(a, st);
 }
@@ -356,7 +345,7 @@ FfnLayout ffn_layout(const FfnShape &s, bool bwd) {
       p[i].nsrc = nsrc;
     }
     const Cut c = f32 ? cut_products<EPI, true>(p, nprob, s.ldf()) : cut_products<EPI, false>(p, nprob, s.ldf());
-    return size_t(c.part_bytes());
+    return c.part_bytes();
   };
   std::integral_constant<int, kStore> store;
   size_t part = 0;

@@ -41,15 +41,16 @@ struct FfnProb {               // one product C (m x n) = sum over sources of A 
 };
 
 // A launch's tiles (those of all its products, with `slabs` slabs of k each): the
-// first `whole` are a block's each. The slabs of the `tail` others are laid end
-// to end and cut into `cuts` runs of `run`, a block's each: a launch ends with
-// all CUs at work, however few tiles it has. A block that holds a part of a tile
-// stores its fp32 sums; block c and tail tile t share slot c + t (along the
-// runs one of the two grows at a time), and k_tail adds a tile's slots in order.
+// first `whole` are a block's each. The `tail` others are cut along k into `parts`
+// parts of `per` slabs, a block's each, the first parts of all of them ahead of
+// the second ones: blocks that run together work on the same k and share operand
+// panels in L2. (Cut end to end into runs of equal length, whatever their k, the
+// weight gradients of 16384 x 1536 x 6144 took 2.66 us a slab instead of 1.73.)
+// A part's block stores its fp32 sums, and k_tail adds a tile's parts in order.
 struct FfnArgs {
   FfnProb p[3];
   int32_t nprob, act;
-  int32_t whole, tail, slabs, run, cuts;
+  int32_t whole, tail, slabs, parts, per;
   float *part;
   int32_t ldf;                 // row length of the inner tensors
   void *sa, *sb;               // a, b as kept for the backward pass (kAct: may be null)
@@ -58,13 +59,12 @@ struct FfnArgs {
   int64_t plane;               // bytes from one plane of h, da, db to the next
 };
 
-// act(a) and its derivative. fp32 results take the accurate exponential and
-// division; for bf16 results the hardware's (errors near 2^-20) are far below
-// the rounding that follows.
+// act(a) and its derivative. fp32 results take the accurate exponential; for bf16
+// results the hardware's (errors near 2^-20) is far below the rounding that
+// follows.
 template <bool F32>
 __device__ __forceinline__ float sigmoid(float a) {
-  if constexpr (F32) return 1.0f / (1.0f + expf(-a));
-  return __builtin_amdgcn_rcpf(1.0f + __expf(-a));
+  return __builtin_amdgcn_rcpf(1.0f + (F32 ? expf(-a) : __expf(-a)));
 }
 template <bool F32>
 __device__ __forceinline__ void act_and_slope(int act, float a, float &f, float &s) {
@@ -84,43 +84,31 @@ __device__ __forceinline__ void act_and_slope(int act, float a, float &f, float 
   }
 }
 
-// The three planes of fp32 values: each is the nearest bf16 number to what the
-// ones before it leave (the largest finite one where that would be infinity).
-__device__ __forceinline__ uint16_t bf16_near(float v) {
-  const uint32_t u = __float_as_uint(v);
-  if ((u & 0x7f800000u) == 0x7f800000u) return f32_to_bf16(v);
-  uint16_t r = f32_to_bf16(v);
-  return (r & 0x7fffu) == 0x7f80u ? uint16_t(r - 1) : r;
-}
-__device__ __forceinline__ void planes_of(float v, uint16_t (&p)[3]) {
-  p[0] = bf16_near(v);
-  float r = v - to_f(p[0]);
-  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) r = 0.0f;
-  p[1] = f32_to_bf16(r);
-  p[2] = f32_to_bf16(r - to_f(p[1]));
-}
-
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
-// 8 values as bf16 (one rounding) or as three planes `plane` bytes apart.
+// 8 values as bf16 (one rounding), or as three planes `plane` bytes apart: each is
+// the nearest bf16 number to what the ones before it leave (the first one held
+// to the finite range, so that the largest fp32 values leave something finite; an
+// infinity or a NaN stays one in the second plane).
 template <bool F32>
 __device__ __forceinline__ void store_planes(char *p, int64_t plane, const float (&v)[8]) {
-  if constexpr (!F32) {
-    floatx8 f;
+  floatx8 f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = v[j];
+  for (int j = 0; j < 8; ++j) f[j] = v[j];
+  if constexpr (!F32) {
     *reinterpret_cast<bf16x8 *>(p) = __builtin_convertvector(f, bf16x8);
   } else {
-    u16x8 q[3];
+    constexpr float kMost = 3.38953139e38f;            // the largest bf16 number
+    floatx8 c;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint16_t t[3];
-      planes_of(v[j], t);
+    for (int j = 0; j < 8; ++j) c[j] = fminf(fmaxf(f[j], -kMost), kMost);
 #pragma unroll
-      for (int c = 0; c < 3; ++c) q[c][j] = t[c];
+    for (int q = 0; q < 3; ++q) {
+      const bf16x8 h = __builtin_convertvector(q == 0 ? c : f, bf16x8);
+      *reinterpret_cast<bf16x8 *>(p + q * plane) = h;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] -= float(h[j]);
     }
-#pragma unroll
-    for (int c = 0; c < 3; ++c) *reinterpret_cast<u16x8 *>(p + c * plane) = q[c];
   }
 }
 
@@ -323,24 +311,26 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
   const int lr = lane & 31, lk = lane >> 5;
   const int wm = wave / WGN, wn = wave % WGN;
 
-  // Block -> tile, or run of the tail: each XCD (block index modulo 8; `whole` is
-  // a multiple of 8) takes consecutive ones, in which 8 tiles of one column of
-  // tiles follow each other, so the blocks of an XCD share operand panels in its
-  // L2.
+  // Block -> tile, or part of a tail tile: each XCD (block index modulo 8; `whole`
+  // is a multiple of 8 where there is a tail) takes consecutive ones, in which 8
+  // tiles of one column of tiles follow each other, so the blocks of an XCD share
+  // operand panels in its L2.
   auto by_xcd = [](int b, int n) {
     const int xcd = b & 7, per = n >> 3, rem = n & 7;
     return xcd * per + min(xcd, rem) + (b >> 3);
   };
-  const bool in_tail = int(blockIdx.x) >= args.whole;
-  const int cut = in_tail ? by_xcd(int(blockIdx.x) - args.whole, args.cuts) : 0;
-  int64_t pos = in_tail ? int64_t(cut) * args.run : int64_t(by_xcd(int(blockIdx.x), args.whole)) * args.slabs;
-  const int64_t end = in_tail ? min(pos + args.run, int64_t(args.tail) * args.slabs) : pos + args.slabs;
-  // (a block of no slabs, k = 0, stores its tile's zeros)
-  for (bool once = true; once || pos < end; once = false) {
-  const int tt = args.slabs ? int(pos / args.slabs) : in_tail ? cut : by_xcd(int(blockIdx.x), args.whole);
-  const int s0 = int(pos - int64_t(tt) * args.slabs), s1 = int(min(int64_t(args.slabs), s0 + end - pos)), ns = s1 - s0;
-  pos += ns;
-  const int tile = in_tail ? args.whole + tt : tt;
+  const bool part = int(blockIdx.x) >= args.whole;
+  int tile, s0 = 0, s1 = args.slabs, slot = 0;
+  if (part) {
+    slot = by_xcd(int(blockIdx.x) - args.whole, args.tail * args.parts);
+    const int q = slot / args.tail;
+    tile = args.whole + slot - q * args.tail;
+    s0 = q * args.per;
+    s1 = min(args.slabs, s0 + args.per);
+  } else {
+    tile = by_xcd(int(blockIdx.x), args.whole);
+  }
+  const int ns = s1 - s0;
   FfnProb pr = args.p[0];
   if (args.nprob > 1 && tile >= args.p[1].tile0) pr = args.p[1];
   if (args.nprob > 2 && tile >= args.p[2].tile0) pr = args.p[2];
@@ -474,7 +464,6 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
             float4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
     __builtin_amdgcn_wave_barrier();
     const int row0 = wm * S::WTM + i * 32;
-    const bool part = ns < args.slabs;
     constexpr int PC = EPI == kAct ? 4 : 8;               // 8-column pieces per row
     constexpr int kTasks = 32 * PC / 64;
     constexpr int kCopies = F32 && EPI != kStore ? 1 : kTasks;   // fp32 activations are long code
@@ -491,7 +480,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
       staged(cl, v);
       if constexpr (EPI == kAct) staged(32 + cl, b);
       if (part) {
-        const int64_t at = (int64_t(cut + tt) * BM + row0 + rl) * BN + wn * 64 + cl;
+        const int64_t at = (int64_t(slot) * BM + row0 + rl) * BN + wn * 64 + cl;
         store_whole<true>(args.part, at, v);
         if constexpr (EPI == kAct) store_whole<true>(args.part, at + 32, b);
       } else {
@@ -500,8 +489,6 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
     }
     __builtin_amdgcn_wave_barrier();
   }
-  if (pos < end) __syncthreads();    // the next tile's slabs go where the sums were staged
-  }
 }
 
 // The sums of a tail tile's parts, in the order of k, and what becomes of them.
@@ -509,9 +496,6 @@ template <int BM, int BN, int EPI, bool F32>
 __global__ __launch_bounds__(256) void k_tail(FfnArgs args) {
   constexpr int PC = EPI == kAct ? BN / 16 : BN / 8;      // pieces per tile row
   const int tt = blockIdx.y, tile = args.whole + tt;
-  const int64_t start = int64_t(tt) * args.slabs, last = start + args.slabs - 1;
-  const int c0 = int(start / args.run), c1 = int(last / args.run);
-  if (c0 == c1) return;                                   // one block had the whole tile
   FfnProb pr = args.p[0];
   if (args.nprob > 1 && tile >= args.p[1].tile0) pr = args.p[1];
   if (args.nprob > 2 && tile >= args.p[2].tile0) pr = args.p[2];
@@ -522,8 +506,8 @@ __global__ __launch_bounds__(256) void k_tail(FfnArgs args) {
   // kAct: piece q is columns 8 q of h; its a and b sums lie 32 columns apart
   const int col = EPI == kAct ? (q >> 2) * 64 + (q & 3) * 8 : q * 8;
   float v[8] = {}, b[8] = {};
-  for (int c = c0; c <= c1; ++c) {
-    const int64_t at = (int64_t(c + tt) * BM + row) * BN + col;
+  for (int c = 0; c < args.parts; ++c) {
+    const int64_t at = ((int64_t(c) * args.tail + tt) * BM + row) * BN + col;
     float w[8];
     load_whole<true>(args.part, at, w);
 #pragma unroll
