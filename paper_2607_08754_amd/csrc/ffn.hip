@@ -155,15 +155,18 @@ void launch_products(FfnArgs &a, hipStream_t st) {
   else launch_tiles<kTile, 2, 2, AK, BK, EPI, F32>(a, st);
 }
 
-// The state's parts: a, b, and in bf16 a byte per 8 values of each.
+// The state's parts: a, b, and in bf16 their exponents (16 bytes per row and 128
+// columns).
+size_t exponents(const FfnShape &s) {
+  return s.dtype == SLORR_BF16 ? size_t(cdiv(s.ldf(), 128)) * size_t(s.tokens) * 16 : 0;
+}
 void state_parts(const FfnShape &s, void *state, FfnArgs &a) {
   if (!state) return;
-  const int64_t n = s.tokens * s.ldf();
+  const size_t n = size_t(s.tokens) * size_t(s.ldf()) * s.elem();
   char *p = static_cast<char *>(state);
-  a.sa = p;
-  a.sb = p + n * s.elem();
-  a.ea = reinterpret_cast<uint8_t *>(p) + 2 * n * s.elem();
-  a.eb = a.ea + n / 8;
+  uint8_t *e = reinterpret_cast<uint8_t *>(p) + 2 * n;
+  a.a = {p, e, s.tokens, int32_t(s.ldf())};
+  a.b = {p + n, e + exponents(s), s.tokens, int32_t(s.ldf())};
 }
 
 // An operand as the products read it.
@@ -363,8 +366,7 @@ FfnLayout ffn_layout(const FfnShape &s, bool bwd) {
 }
 
 size_t ffn_state_bytes(const FfnShape &s) {
-  const size_t n = size_t(s.tokens) * size_t(s.ldf());
-  return std::max(size_t(256), 2 * n * s.elem() + (s.dtype == SLORR_BF16 ? n / 4 : 0));
+  return std::max(size_t(256), 2 * (size_t(s.tokens) * size_t(s.ldf()) * s.elem() + exponents(s)));
 }
 
 void enqueue_ffn_forward(const FfnShape &s, const void *x, const void *wg, const void *wu, const void *wd, void *y,

@@ -40,25 +40,6 @@ struct FfnProb {               // one product C (m x n) = sum over sources of A 
   int64_t ldo;
 };
 
-// A launch's tiles (those of all its products, with `slabs` slabs of k each): the
-// first `whole` are a block's each. The `tail` others are cut along k into `parts`
-// parts of `per` slabs, a block's each, the first parts of all of them ahead of
-// the second ones: blocks that run together work on the same k and share operand
-// panels in L2. (Cut end to end into runs of equal length, whatever their k, the
-// weight gradients of 16384 x 1536 x 6144 took 2.66 us a slab instead of 1.73.)
-// A part's block stores its fp32 sums, and k_tail adds a tile's parts in order.
-struct FfnArgs {
-  FfnProb p[3];
-  int32_t nprob, act;
-  int32_t whole, tail, slabs, parts, per;
-  float *part;
-  int32_t ldf;                 // row length of the inner tensors
-  void *sa, *sb;               // a, b as kept for the backward pass (kAct: may be null)
-  uint8_t *ea, *eb;            // their exponents (bf16 tensors)
-  char *h, *da, *db;           // bf16 planes
-  int64_t plane;               // bytes from one plane of h, da, db to the next
-};
-
 // act(a) and its derivative. fp32 results take the accurate exponential; for bf16
 // results the hardware's (errors near 2^-20) is far below the rounding that
 // follows.
@@ -142,10 +123,22 @@ __device__ __forceinline__ void load_whole(const void *base, int64_t at, float (
 // x 1536 x 6144 are off by 3.5e-3 of their size with it; one rounding of the
 // exact ones is 1.7e-3). Eight values with an infinity or a NaN among them are
 // kept in bf16, marked by the exponent 255.
+// The exponents of a row's 128 columns lie together, those of the next row's same
+// columns behind them: what a tile writes and reads of them is contiguous.
+struct Kept {
+  void *v;                     // a or b: rows of ldf values
+  uint8_t *e;
+  int64_t rows;
+  int32_t ldf;
+  __device__ __forceinline__ int64_t at(int row, int col) const { return int64_t(row) * ldf + col; }
+  __device__ __forceinline__ int64_t exp_at(int row, int col) const {
+    return (int64_t(col >> 7) * rows + row) * 16 + ((col & 127) >> 3);
+  }
+};
 template <bool F32>
-__device__ __forceinline__ void store_kept(void *base, uint8_t *exps, int64_t at, const float (&v)[8]) {
+__device__ __forceinline__ void store_kept(const Kept &k, int row, int col, const float (&v)[8]) {
   if constexpr (F32) {
-    store_whole<true>(base, at, v);
+    store_whole<true>(k.v, k.at(row, col), v);
   } else {
     uint32_t m = 0;
 #pragma unroll
@@ -159,26 +152,40 @@ __device__ __forceinline__ void store_kept(void *base, uint8_t *exps, int64_t at
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[j] = uint16_t(int16_t(min(rintf(ldexpf(v[j], 141 - e)), 32767.0f)));
     }
-    *reinterpret_cast<u16x8 *>(static_cast<uint16_t *>(base) + at) = q;
-    exps[at >> 3] = uint8_t(e);
+    // (not read before the backward pass: the caches keep what this launch and the
+    // next one read)
+    __builtin_nontemporal_store(q, reinterpret_cast<u16x8 *>(static_cast<uint16_t *>(k.v) + k.at(row, col)));
+    k.e[k.exp_at(row, col)] = uint8_t(e);
   }
 }
+// Eight kept values as loaded, for a load issued ahead of its use.
 template <bool F32>
-__device__ __forceinline__ void load_kept(const void *base, const uint8_t *exps, int64_t at, float (&v)[8]) {
-  if constexpr (F32) {
-    load_whole<true>(base, at, v);
-  } else {
-    const u16x8 q = *reinterpret_cast<const u16x8 *>(static_cast<const uint16_t *>(base) + at);
-    const int e = exps[at >> 3];
-    if (e == 255) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = to_f(bf16_t(q[j]));
+struct KeptRaw {
+  u32x4 q[F32 ? 2 : 1];
+  uint32_t e;
+  __device__ __forceinline__ void load(const Kept &k, int row, int col) {
+    if constexpr (F32) {
+      const float *p = static_cast<const float *>(k.v) + k.at(row, col);
+      q[0] = gload16(p);
+      q[1] = gload16(p + 4);
     } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = ldexpf(float(int16_t(q[j])), e - 141);
+      q[0] = gload16(static_cast<const uint16_t *>(k.v) + k.at(row, col));
+      e = *(const SLORR_GLOBAL uint8_t *)(k.e + k.exp_at(row, col));
     }
   }
-}
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    if constexpr (F32) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(q[j >> 2][j & 3]);
+    } else if (e == 255) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = to_f(bf16_t(q[0][j >> 1] >> (16 * (j & 1))));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = ldexpf(float(int16_t(q[0][j >> 1] >> (16 * (j & 1)))), int(e) - 141);
+    }
+  }
+};
 // the first n of 8 values (8: whole when the address allows it)
 template <bool F32>
 __device__ __forceinline__ void store_some(void *base, int64_t at, int n, const float (&v)[8]) {
@@ -192,6 +199,24 @@ __device__ __forceinline__ void store_some(void *base, int64_t at, int n, const 
   for (int j = 0; j < 8; ++j)
     if (j < n) p[j] = from_f<T>(v[j]);
 }
+
+// A launch's tiles (those of all its products, with `slabs` slabs of k each): the
+// first `whole` are a block's each. The `tail` others are cut along k into `parts`
+// parts of `per` slabs, a block's each, the first parts of all of them ahead of
+// the second ones: blocks that run together work on the same k and share operand
+// panels in L2. (Cut end to end into runs of equal length, whatever their k, the
+// weight gradients of 16384 x 1536 x 6144 took 2.66 us a slab instead of 1.73.)
+// A part's block stores its fp32 sums, and k_tail adds a tile's parts in order.
+struct FfnArgs {
+  FfnProb p[3];
+  int32_t nprob, act;
+  int32_t whole, tail, slabs, parts, per;
+  float *part;
+  int32_t ldf;                 // row length of the inner tensors
+  Kept a, b;                   // as kept for the backward pass (kAct: v may be null)
+  char *h, *da, *db;           // bf16 planes
+  int64_t plane;               // bytes from one plane of h, da, db to the next
+};
 
 // ---------------------------------------------------------------------------
 // Block tile BM x BN, wave tiles of FM x FN MFMA tiles of 32 x 32, slabs of 64
@@ -261,9 +286,20 @@ __device__ __forceinline__ void tile_corner(const FfnProb &p, int t, int &m0, in
 
 // What becomes of 8 consecutive sums v of row `row` from column `col` on; kAct: of
 // a's (v) and b's.
+// kActBack: `kept`, a and b there.
+template <bool F32>
+struct KeptPair {
+  KeptRaw<F32> a, b;
+  __device__ __forceinline__ void load(const FfnArgs &args, int rows, int row, int col) {
+    if (row < rows && col < args.ldf) {
+      a.load(args.a, row, col);
+      b.load(args.b, row, col);
+    }
+  }
+};
 template <int EPI, bool F32>
 __device__ __forceinline__ void finish(const FfnArgs &args, const FfnProb &pr, int row, int col, float (&v)[8],
-                                       float (&b)[8]) {
+                                       float (&b)[8], const KeptPair<F32> &kept) {
   if (row >= pr.m) return;
   if constexpr (EPI == kStore) {
     if (col < pr.n) store_some<F32>(pr.out, int64_t(row) * pr.ldo + col, pr.n - col, v);
@@ -273,9 +309,9 @@ __device__ __forceinline__ void finish(const FfnArgs &args, const FfnProb &pr, i
   const int64_t at = int64_t(row) * args.ldf + col;
   float h[8];
   if constexpr (EPI == kAct) {
-    if (args.sa) {
-      store_kept<F32>(args.sa, args.ea, at, v);
-      store_kept<F32>(args.sb, args.eb, at, b);
+    if (args.a.v) {
+      store_kept<F32>(args.a, row, col, v);
+      store_kept<F32>(args.b, row, col, b);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -286,8 +322,8 @@ __device__ __forceinline__ void finish(const FfnArgs &args, const FfnProb &pr, i
     store_planes<F32>(args.h + at * 2, args.plane, h);
   } else {
     float a[8], da[8], db[8];
-    load_kept<F32>(args.sa, args.ea, at, a);
-    load_kept<F32>(args.sb, args.eb, at, b);
+    kept.a.values(a);
+    kept.b.values(b);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       float f, sl;
@@ -409,6 +445,24 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
+  // kActBack: a and b of a 32-row block of the wave tile are loaded a block ahead,
+  // the first ones before the products (fp32 tensors: with the block, there are
+  // no registers for more)
+  constexpr int PC = EPI == kAct ? 4 : 8;                 // 8-column pieces per row
+  constexpr int kTasks = 32 * PC / 64;
+  constexpr int kAhead = F32 ? 0 : 1;
+  KeptPair<F32> kept[EPI == kActBack ? kAhead + 1 : 1][EPI == kActBack ? kTasks : 1];
+  auto kept_load = [&](int i) {
+    if constexpr (EPI == kActBack) {
+#pragma unroll
+      for (int t = 0; t < kTasks; ++t) {
+        const int task = lane + 64 * t;
+        kept[kAhead ? i & 1 : 0][t].load(args, pr.m, m0 + wm * S::WTM + i * 32 + task / PC, n0 + wn * 64 + (task % PC) * 8);
+      }
+    }
+  };
+  if (kAhead && !part) kept_load(0);
+
 #pragma unroll
   for (int q = 0; q < NS - 1; ++q)
     if (q < ns) dload(q);
@@ -464,8 +518,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
             float4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
     __builtin_amdgcn_wave_barrier();
     const int row0 = wm * S::WTM + i * 32;
-    constexpr int PC = EPI == kAct ? 4 : 8;               // 8-column pieces per row
-    constexpr int kTasks = 32 * PC / 64;
+    if (kAhead && i + 1 < FM && !part) kept_load(i + 1);
     constexpr int kCopies = F32 && EPI != kStore ? 1 : kTasks;   // fp32 activations are long code
 #pragma unroll kCopies
     for (int t = 0; t < kTasks; ++t) {
@@ -484,7 +537,13 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
         store_whole<true>(args.part, at, v);
         if constexpr (EPI == kAct) store_whole<true>(args.part, at + 32, b);
       } else {
-        finish<EPI, F32>(args, pr, m0 + row0 + rl, n0 + wn * (EPI == kAct ? 32 : 64) + cl, v, b);
+        KeptPair<F32> k;
+        if constexpr (EPI == kActBack) {
+          // (the rolled loop of fp32 tensors cannot name its registers)
+          if constexpr (kCopies == 1) k.load(args, pr.m, m0 + row0 + rl, n0 + wn * 64 + cl);
+          else k = kept[kAhead ? i & 1 : 0][t];
+        }
+        finish<EPI, F32>(args, pr, m0 + row0 + rl, n0 + wn * (EPI == kAct ? 32 : 64) + cl, v, b, k);
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -518,7 +577,9 @@ __global__ __launch_bounds__(256) void k_tail(FfnArgs args) {
       for (int j = 0; j < 8; ++j) b[j] += w[j];
     }
   }
-  finish<EPI, F32>(args, pr, m0 + row, n0 + q * 8, v, b);
+  KeptPair<F32> kept;
+  if constexpr (EPI == kActBack) kept.load(args, pr.m, m0 + row, n0 + q * 8);
+  finish<EPI, F32>(args, pr, m0 + row, n0 + q * 8, v, b, kept);
 }
 
 // ---------------------------------------------------------------------------
