@@ -173,20 +173,19 @@ template <int N, int kLdsStep>
 __device__ __forceinline__ void fetch_run(i32x4 rsrc, uint32_t voff, uint32_t soff_step, uint32_t lds_base) {
   static_assert(N == 2 || N == 4 || N == 8, "fetches in a row");
 #if defined(__HIP_DEVICE_COMPILE__)
-  const uint32_t m = __builtin_amdgcn_readfirstlane(lds_base);
+  uint32_t m = __builtin_amdgcn_readfirstlane(lds_base), so = 0;
   const uint32_t step = __builtin_amdgcn_readfirstlane(soff_step);
-  uint32_t so = 0;
-#define SLORR_FETCH "buffer_load_dwordx4 %1, %2, %0 offen lds\n\t"
+#define SLORR_FETCH "buffer_load_dwordx4 %2, %3, %0 offen lds\n\t"
 #define SLORR_NEXT "s_add_u32 m0, m0, %5\n\ts_add_u32 %0, %0, %4\n\t" SLORR_FETCH
-#define SLORR_FIRST "s_mov_b32 m0, %3\n\ts_nop 4\n\t" SLORR_FETCH
+#define SLORR_FIRST "s_nop 4\n\t" SLORR_FETCH
   if constexpr (N == 2)
-    asm volatile(SLORR_FIRST SLORR_NEXT : "+&s"(so) : "v"(voff), "s"(rsrc), "s"(m), "s"(step), "n"(kLdsStep) : "memory", "m0", "scc");
+    asm volatile(SLORR_FIRST SLORR_NEXT : "+&s"(so), "+{m0}"(m) : "v"(voff), "s"(rsrc), "s"(step), "n"(kLdsStep) : "memory", "scc");
   else if constexpr (N == 4)
     asm volatile(SLORR_FIRST SLORR_NEXT SLORR_NEXT SLORR_NEXT
-                 : "+&s"(so) : "v"(voff), "s"(rsrc), "s"(m), "s"(step), "n"(kLdsStep) : "memory", "m0", "scc");
+                 : "+&s"(so), "+{m0}"(m) : "v"(voff), "s"(rsrc), "s"(step), "n"(kLdsStep) : "memory", "scc");
   else
     asm volatile(SLORR_FIRST SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT SLORR_NEXT
-                 : "+&s"(so) : "v"(voff), "s"(rsrc), "s"(m), "s"(step), "n"(kLdsStep) : "memory", "m0", "scc");
+                 : "+&s"(so), "+{m0}"(m) : "v"(voff), "s"(rsrc), "s"(step), "n"(kLdsStep) : "memory", "scc");
 #undef SLORR_FETCH
 #undef SLORR_NEXT
 #undef SLORR_FIRST

@@ -67,70 +67,91 @@ __global__ __launch_bounds__(256) void k_planes(LayArgs args) {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a launch's products are cut: tiles of 256 or 128, how many of them whole,
-// and the parts of the others.
+// The block tiles: 256 x 256 (8 waves of 128 x 64), 256 x 128 (8 of 64 x 64, three
+// LDS stages) and 128 x 128 (4 of 64 x 64, two blocks per CU). Microseconds of a
+// round of blocks: per slab of k with every CU at work (alone: with one block of
+// the smallest per CU at most, where a slab's latency is all there is), and for
+// its start and end (kActBack, which loads and stores five values per sum: back).
+// From 16384 x 1536 x 6144 in bf16, us of the three tiles: the weight gradients'
+// 256 slabs 467, 288 and 276 a round, y's 96 slabs 184, 118 and 119, dh's 24 slabs
+// 87, 46 and 47 (a round of the first is twice the work of the others').
+struct TileKind {
+  int bm, bn, slots;
+  double slab, alone, ends, back;
+};
+constexpr TileKind kTiles[] = {{256, 256, kCus, 1.77, 1.77, 13, 44},
+                               {256, 128, kCus, 1.15, 1.15, 10, 20},
+                               {128, 128, 2 * kCus, 1.15, 0.75, 4, 18}};
+constexpr double kPartByte = 2 / 4.5e6;                   // a part's sums, written and read once at 4.5 TB/s
+constexpr double kTailLaunch = 5;
+
+// How a launch's products are cut: the tile, how many of them whole, and the
+// parts of the others.
 struct Cut {
-  int tile = 0;
+  int kind = -1;
   int64_t whole = 0, tail = 0, parts = 0, per = 0;
-  size_t part_bytes() const { return size_t(tail * parts) * size_t(tile) * size_t(tile) * 4; }
+  size_t part_bytes() const {
+    return kind < 0 ? 0 : size_t(tail * parts) * size_t(kTiles[kind].bm) * size_t(kTiles[kind].bn) * 4;
+  }
 };
 
-// Microseconds per slab of a round of tiles with every CU at work (1536 x 6144,
-// 16384 tokens, bf16: one 256-tile per CU, or two 128-tiles), and with one
-// 128-tile per CU at most, where a slab's latency is all there is; and per byte
-// of the parts, written and read once (4.5 TB/s).
-constexpr double kSlab256 = 1.75, kSlab128 = 1.35, kSlabAlone = 0.8, kPartByte = 2 / 4.5e6;
+template <int EPI>
+int64_t tiles_m(const FfnProb &p, const TileKind &k) { return cdiv(p.m, k.bm); }
+template <int EPI>
+int64_t tiles_n(const FfnProb &p, const TileKind &k, int64_t ldf) {
+  return EPI == kStore ? cdiv(p.n, k.bn) : cdiv(ldf, EPI == kAct ? k.bn / 2 : k.bn);
+}
 
-// The least of: rounds of whole tiles; whole tiles as long as they fill rounds,
-// the rest cut into parts. 16384 x 1536 x 6144, one 256-tile per CU: y's 384
-// tiles of 96 slabs, two rounds whole 428 us, the last 128 in two parts each 348
-// + 17 us; dx (192 slabs) 701 and 560 + 17. 501 x 1280 x 3456, forward: 68 and 45 us.
+// The least of, over the tiles: rounds of whole tiles; whole tiles as long as they
+// fill rounds, the rest cut into parts.
 template <int EPI, bool F32>
 Cut cut_products(const FfnProb *p, int nprob, int64_t ldf) {
   Cut best;
   double least = 0;
   const int64_t slabs = cdiv(p[0].k, 64) * p[0].nsrc * (F32 ? 6 : 1);
-  for (int tile : {kBigTile, kTile}) {
-    const int64_t slots = tile == kBigTile ? kCus : 2 * kCus;
-    auto round = [&](int64_t units) { return tile == kBigTile ? kSlab256 : units > kCus ? kSlab128 : kSlabAlone; };
-    auto time = [&](int64_t units, int64_t n) {           // units of n slabs
-      const int64_t full = units / slots, rest = units - full * slots;
-      return double(n) * (double(full) * round(slots) + (rest ? round(rest) : 0.0));
+  for (int kind = 0; kind < 3; ++kind) {
+    const TileKind &k = kTiles[kind];
+    // units of n slabs
+    auto time = [&](int64_t units, int64_t n, double ends) {
+      const int64_t full = units / k.slots, rest = units - full * k.slots;
+      return double(full) * (double(n) * k.slab + ends) + (rest ? double(n) * (rest > kCus ? k.slab : k.alone) + ends : 0.0);
     };
+    const double ends = EPI == kActBack ? k.back : k.ends;
     int64_t tiles = 0;
-    for (int i = 0; i < nprob; ++i)
-      tiles += cdiv(p[i].m, tile) * cdiv(EPI == kStore ? p[i].n : ldf, EPI == kAct ? tile / 2 : tile);
+    for (int i = 0; i < nprob; ++i) tiles += tiles_m<EPI>(p[i], k) * tiles_n<EPI>(p[i], k, ldf);
     auto offer = [&](const Cut &c, double t) {
-      if (!best.tile || t < least) {
+      if (best.kind < 0 || t < least) {
         best = c;
         least = t;
       }
     };
     Cut c;
-    c.tile = tile;
+    c.kind = kind;
     c.whole = tiles;
-    offer(c, time(tiles, slabs));
-    c.whole = tiles / slots * slots;
+    offer(c, time(tiles, slabs, ends));
+    c.whole = tiles / k.slots * k.slots;
     c.tail = tiles - c.whole;
     // parts of at least 4 slabs: below, a block's start and its part's way through
     // memory cost more than the slabs
     for (c.parts = 2; c.tail && c.parts <= 16 && cdiv(slabs, c.parts) >= 4; ++c.parts) {
       c.per = cdiv(slabs, c.parts);
       if (c.per * (c.parts - 1) >= slabs) continue;       // (the last part would be empty)
-      offer(c, time(c.whole, slabs) + time(c.tail * c.parts, c.per) + 5.0 + double(c.part_bytes()) * kPartByte);
+      offer(c, time(c.whole, slabs, ends) + time(c.tail * c.parts, c.per, k.ends) + kTailLaunch +
+                   double(c.part_bytes()) * kPartByte);
     }
   }
   return best;
 }
 
-template <int B, int WGM, int WGN, bool AK, bool BK, int EPI, bool F32>
+template <int KIND, int WGM, int WGN, int NS, bool AK, bool BK, int EPI, bool F32>
 void launch_tiles(const FfnArgs &a, hipStream_t st) {
+  constexpr int BM = kTiles[KIND].bm, BN = kTiles[KIND].bn;
   const dim3 grid(uint32_t(a.whole + a.tail * a.parts));
-  hipLaunchKernelGGL((k_ffn<B, B, WGM, WGN, 2, AK, BK, EPI, F32>), grid, dim3(64 * WGM * WGN), 0, st, a);
+  hipLaunchKernelGGL((k_ffn<BM, BN, WGM, WGN, NS, AK, BK, EPI, F32>), grid, dim3(64 * WGM * WGN), 0, st, a);
   check(hipGetLastError(), "kernel launch");
   if (!a.tail) return;
-  const dim3 pieces(uint32_t(B * B / (EPI == kAct ? 16 : 8) / 256), uint32_t(a.tail));
-  hipLaunchKernelGGL((k_tail<B, B, EPI, F32>), pieces, dim3(256), 0, st, a);
+  const dim3 pieces(uint32_t(BM * BN / (EPI == kAct ? 16 : 8) / 256), uint32_t(a.tail));
+  hipLaunchKernelGGL((k_tail<BM, BN, EPI, F32>), pieces, dim3(256), 0, st, a);
   check(hipGetLastError(), "kernel launch");
 }
 
@@ -140,8 +161,8 @@ void launch_products(FfnArgs &a, hipStream_t st) {
   int64_t tiles = 0;
   for (int i = 0; i < a.nprob; ++i) {
     FfnProb &p = a.p[i];
-    p.tm = int32_t(cdiv(p.m, c.tile));
-    p.tn = int32_t(cdiv(EPI == kStore ? p.n : a.ldf, EPI == kAct ? c.tile / 2 : c.tile));
+    p.tm = int32_t(tiles_m<EPI>(p, kTiles[c.kind]));
+    p.tn = int32_t(tiles_n<EPI>(p, kTiles[c.kind], a.ldf));
     p.tile0 = int32_t(tiles);
     tiles += int64_t(p.tm) * p.tn;
   }
@@ -151,8 +172,9 @@ void launch_products(FfnArgs &a, hipStream_t st) {
   a.slabs = int32_t(cdiv(a.p[0].k, 64)) * a.p[0].nsrc * (F32 ? 6 : 1);
   a.parts = int32_t(c.parts);
   a.per = int32_t(c.per);
-  if (c.tile == kBigTile) launch_tiles<kBigTile, 2, 4, AK, BK, EPI, F32>(a, st);
-  else launch_tiles<kTile, 2, 2, AK, BK, EPI, F32>(a, st);
+  if (c.kind == 0) launch_tiles<0, 2, 4, 2, AK, BK, EPI, F32>(a, st);
+  else if (c.kind == 1) launch_tiles<1, 4, 2, 3, AK, BK, EPI, F32>(a, st);
+  else launch_tiles<2, 2, 2, 2, AK, BK, EPI, F32>(a, st);
 }
 
 // The state's parts: a, b, and in bf16 their exponents (16 bytes per row and 128
@@ -335,30 +357,33 @@ FfnLayout ffn_layout(const FfnShape &s, bool bwd) {
     l.db = take(T * size_t(s.ldf()) * pl);
   }
   // parts of cut tiles: what the launches of the call need at most (the weight
-  // gradients that are asked for are a launch of one to three products)
+  // gradients that are asked for are a launch: `same` of inner x dim, `other` of
+  // dim x inner)
   const bool f32 = s.dtype == SLORR_F32;
-  auto need = [&](auto epi, int nprob, int64_t m, int64_t n, int64_t k, int nsrc) {
+  auto need = [&](auto epi, int same, int other, int64_t m, int64_t n, int64_t k, int nsrc) {
     constexpr int EPI = decltype(epi)::value;
     FfnProb p[3]{};
-    for (int i = 0; i < nprob; ++i) {
-      // (dw_down's m and n change places: with square tiles the number is the same)
-      p[i].m = int32_t(m);
-      p[i].n = int32_t(n);
+    for (int i = 0; i < same + other; ++i) {
+      p[i].m = int32_t(i < same ? m : n);
+      p[i].n = int32_t(i < same ? n : m);
       p[i].k = int32_t(k);
       p[i].nsrc = nsrc;
     }
+    const int nprob = same + other;
     const Cut c = f32 ? cut_products<EPI, true>(p, nprob, s.ldf()) : cut_products<EPI, false>(p, nprob, s.ldf());
     return c.part_bytes();
   };
   std::integral_constant<int, kStore> store;
   size_t part = 0;
   if (!bwd) {
-    part = std::max(need(std::integral_constant<int, kAct>{}, 1, s.tokens, s.inner, s.dim, 1),
-                    need(store, 1, s.tokens, s.dim, s.inner, 1));
+    part = std::max(need(std::integral_constant<int, kAct>{}, 1, 0, s.tokens, s.inner, s.dim, 1),
+                    need(store, 1, 0, s.tokens, s.dim, s.inner, 1));
   } else {
-    part = std::max(need(std::integral_constant<int, kActBack>{}, 1, s.tokens, s.inner, s.dim, 1),
-                    need(store, 1, s.tokens, s.dim, s.inner, 2));
-    for (int i = 1; i <= 3; ++i) part = std::max(part, need(store, i, s.inner, s.dim, s.tokens, 1));
+    part = std::max(need(std::integral_constant<int, kActBack>{}, 1, 0, s.tokens, s.inner, s.dim, 1),
+                    need(store, 1, 0, s.tokens, s.dim, s.inner, 2));
+    for (int same = 0; same <= 2; ++same)
+      for (int other = 0; other <= 1; ++other)
+        if (same + other) part = std::max(part, need(store, same, other, s.inner, s.dim, s.tokens, 1));
   }
   l.part = take(part);
   l.bytes = std::max(l.bytes, size_t(256));
