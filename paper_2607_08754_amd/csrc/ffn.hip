@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "block.hpp"
+#include "cut.hpp"
 #include "ffn_gemm.hpp"
 #include "layout.hpp"
 
@@ -65,84 +66,6 @@ __global__ __launch_bounds__(256) void k_planes(LayArgs args) {
   }
 }
 
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// The block tiles: 256 x 256 (8 waves of 128 x 64), 256 x 128 (8 of 64 x 64, three
-// LDS stages) and 128 x 128 (4 of 64 x 64, two blocks per CU). Microseconds of a
-// round of blocks: per slab of k with every CU at work (alone: with one block of
-// the smallest per CU at most, where a slab's latency is all there is), and for
-// its start and end (kActBack, which loads and stores five values per sum: back).
-// From 16384 x 1536 x 6144 in bf16, us of the three tiles: the weight gradients'
-// 256 slabs 467, 288 and 276 a round, y's 96 slabs 184, 118 and 119, dh's 24 slabs
-// 87, 46 and 47 (a round of the first is twice the work of the others').
-struct TileKind {
-  int bm, bn, slots;
-  double slab, alone, ends, back;
-};
-constexpr TileKind kTiles[] = {{256, 256, kCus, 1.77, 1.77, 13, 44},
-                               {256, 128, kCus, 1.15, 1.15, 10, 20},
-                               {128, 128, 2 * kCus, 1.15, 0.75, 4, 18}};
-constexpr double kPartByte = 2 / 4.5e6;                   // a part's sums, written and read once at 4.5 TB/s
-constexpr double kTailLaunch = 5;
-
-// How a launch's products are cut: the tile, how many of them whole, and the
-// parts of the others.
-struct Cut {
-  int kind = -1;
-  int64_t whole = 0, tail = 0, parts = 0, per = 0;
-  size_t part_bytes() const {
-    return kind < 0 ? 0 : size_t(tail * parts) * size_t(kTiles[kind].bm) * size_t(kTiles[kind].bn) * 4;
-  }
-};
-
-template <int EPI>
-int64_t tiles_m(const FfnProb &p, const TileKind &k) { return cdiv(p.m, k.bm); }
-template <int EPI>
-int64_t tiles_n(const FfnProb &p, const TileKind &k, int64_t ldf) {
-  return EPI == kStore ? cdiv(p.n, k.bn) : cdiv(ldf, EPI == kAct ? k.bn / 2 : k.bn);
-}
-
-// The least of, over the tiles: rounds of whole tiles; whole tiles as long as they
-// fill rounds, the rest cut into parts.
-template <int EPI, bool F32>
-Cut cut_products(const FfnProb *p, int nprob, int64_t ldf) {
-  Cut best;
-  double least = 0;
-  const int64_t slabs = cdiv(p[0].k, 64) * p[0].nsrc * (F32 ? 6 : 1);
-  for (int kind = 0; kind < 3; ++kind) {
-    const TileKind &k = kTiles[kind];
-    // units of n slabs
-    auto time = [&](int64_t units, int64_t n, double ends) {
-      const int64_t full = units / k.slots, rest = units - full * k.slots;
-      return double(full) * (double(n) * k.slab + ends) + (rest ? double(n) * (rest > kCus ? k.slab : k.alone) + ends : 0.0);
-    };
-    const double ends = EPI == kActBack ? k.back : k.ends;
-    int64_t tiles = 0;
-    for (int i = 0; i < nprob; ++i) tiles += tiles_m<EPI>(p[i], k) * tiles_n<EPI>(p[i], k, ldf);
-    auto offer = [&](const Cut &c, double t) {
-      if (best.kind < 0 || t < least) {
-        best = c;
-        least = t;
-      }
-    };
-    Cut c;
-    c.kind = kind;
-    c.whole = tiles;
-    offer(c, time(tiles, slabs, ends));
-    c.whole = tiles / k.slots * k.slots;
-    c.tail = tiles - c.whole;
-    // parts of at least 4 slabs: below, a block's start and its part's way through
-    // memory cost more than the slabs
-    for (c.parts = 2; c.tail && c.parts <= 16 && cdiv(slabs, c.parts) >= 4; ++c.parts) {
-      c.per = cdiv(slabs, c.parts);
-      if (c.per * (c.parts - 1) >= slabs) continue;       // (the last part would be empty)
-      offer(c, time(c.whole, slabs, ends) + time(c.tail * c.parts, c.per, k.ends) + kTailLaunch +
-                   double(c.part_bytes()) * kPartByte);
-    }
-  }
-  return best;
-}
-
 template <int KIND, int WGM, int WGN, int NS, bool AK, bool BK, int EPI, bool F32>
 void launch_tiles(const FfnArgs &a, hipStream_t st) {
   constexpr int BM = kTiles[KIND].bm, BN = kTiles[KIND].bn;
@@ -157,24 +80,25 @@ void launch_tiles(const FfnArgs &a, hipStream_t st) {
 
 template <bool AK, bool BK, int EPI, bool F32>
 void launch_products(FfnArgs &a, hipStream_t st) {
-  const Cut c = cut_products<EPI, F32>(a.p, a.nprob, a.ldf);
+  Product q[3];
+  for (int i = 0; i < a.nprob; ++i) q[i] = {a.p[i].m, a.p[i].n, a.p[i].k, a.p[i].nsrc};
+  const Cut c = cut_products(q, a.nprob, EPI, F32, a.ldf);
   int64_t tiles = 0;
   for (int i = 0; i < a.nprob; ++i) {
     FfnProb &p = a.p[i];
-    p.tm = int32_t(tiles_m<EPI>(p, kTiles[c.kind]));
-    p.tn = int32_t(tiles_n<EPI>(p, kTiles[c.kind], a.ldf));
+    p.tm = int32_t(tiles_m(q[i], kTiles[c.kind]));
+    p.tn = int32_t(tiles_n(q[i], kTiles[c.kind], EPI, a.ldf));
     p.tile0 = int32_t(tiles);
     tiles += int64_t(p.tm) * p.tn;
   }
   if (!tiles) return;
   a.whole = int32_t(c.whole);
   a.tail = int32_t(c.tail);
-  a.slabs = int32_t(cdiv(a.p[0].k, 64)) * a.p[0].nsrc * (F32 ? 6 : 1);
+  a.slabs = int32_t(slabs_of(q[0], F32));
   a.parts = int32_t(c.parts);
   a.per = int32_t(c.per);
   if (c.kind == 0) launch_tiles<0, 2, 4, 2, AK, BK, EPI, F32>(a, st);
-  else if (c.kind == 1) launch_tiles<1, 4, 2, 3, AK, BK, EPI, F32>(a, st);
-  else launch_tiles<2, 2, 2, 2, AK, BK, EPI, F32>(a, st);
+  else launch_tiles<1, 2, 2, 2, AK, BK, EPI, F32>(a, st);
 }
 
 // The state's parts: a, b, and in bf16 their exponents (16 bytes per row and 128
@@ -356,36 +280,7 @@ FfnLayout ffn_layout(const FfnShape &s, bool bwd) {
     l.da = take(T * size_t(s.ldf()) * pl);
     l.db = take(T * size_t(s.ldf()) * pl);
   }
-  // parts of cut tiles: what the launches of the call need at most (the weight
-  // gradients that are asked for are a launch: `same` of inner x dim, `other` of
-  // dim x inner)
-  const bool f32 = s.dtype == SLORR_F32;
-  auto need = [&](auto epi, int same, int other, int64_t m, int64_t n, int64_t k, int nsrc) {
-    constexpr int EPI = decltype(epi)::value;
-    FfnProb p[3]{};
-    for (int i = 0; i < same + other; ++i) {
-      p[i].m = int32_t(i < same ? m : n);
-      p[i].n = int32_t(i < same ? n : m);
-      p[i].k = int32_t(k);
-      p[i].nsrc = nsrc;
-    }
-    const int nprob = same + other;
-    const Cut c = f32 ? cut_products<EPI, true>(p, nprob, s.ldf()) : cut_products<EPI, false>(p, nprob, s.ldf());
-    return c.part_bytes();
-  };
-  std::integral_constant<int, kStore> store;
-  size_t part = 0;
-  if (!bwd) {
-    part = std::max(need(std::integral_constant<int, kAct>{}, 1, 0, s.tokens, s.inner, s.dim, 1),
-                    need(store, 1, 0, s.tokens, s.dim, s.inner, 1));
-  } else {
-    part = std::max(need(std::integral_constant<int, kActBack>{}, 1, 0, s.tokens, s.inner, s.dim, 1),
-                    need(store, 1, 0, s.tokens, s.dim, s.inner, 2));
-    for (int same = 0; same <= 2; ++same)
-      for (int other = 0; other <= 1; ++other)
-        if (same + other) part = std::max(part, need(store, same, other, s.inner, s.dim, s.tokens, 1));
-  }
-  l.part = take(part);
+  l.part = take(FfnProducts{s.tokens, s.dim, s.inner, s.ldf(), s.dtype == SLORR_F32}.part_bytes(bwd));
   l.bytes = std::max(l.bytes, size_t(256));
   return l;
 }

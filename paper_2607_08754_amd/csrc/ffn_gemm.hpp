@@ -19,6 +19,7 @@
 // products cost 6/16 of one fp32 product. An infinity gives NaN (infinity times
 // a zero plane).
 #pragma once
+#include "cut.hpp"
 #include "device.hpp"
 
 namespace slorr {
@@ -26,8 +27,6 @@ namespace slorr {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float floatx8 __attribute__((ext_vector_type(8)));
-
-enum FfnEpi { kStore = 0, kAct = 1, kActBack = 2 };
 
 struct FfnProb {               // one product C (m x n) = sum over sources of A B^T
   const char *a[2], *b[2];     // sources; kAct: b[0], b[1] are both products' rows, one source
@@ -275,13 +274,13 @@ __device__ __forceinline__ int plane_pair(int i) {
   return int((t >> (4 * i)) & 15u);
 }
 
-// The corner of a product's tile t: 8 tiles of a column of tiles follow each other.
+// The corner of a product's tile t.
 template <int BM, int BN, int EPI>
 __device__ __forceinline__ void tile_corner(const FfnProb &p, int t, int &m0, int &n0) {
-  const int gsize = 8 * p.tn, g = t / gsize, r = t - g * gsize;
-  const int rows = min(8, p.tm - 8 * g), c = r / rows;
-  m0 = (8 * g + r - c * rows) * BM;
-  n0 = c * (EPI == kAct ? BN / 2 : BN);
+  int row, col;
+  tile_place(t, p.tm, p.tn, row, col);
+  m0 = row * BM;
+  n0 = col * (EPI == kAct ? BN / 2 : BN);
 }
 
 // What becomes of 8 consecutive sums v of row `row` from column `col` on; kAct: of
@@ -351,18 +350,12 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
   // is a multiple of 8 where there is a tail) takes consecutive ones, in which 8
   // tiles of one column of tiles follow each other, so the blocks of an XCD share
   // operand panels in its L2.
-  auto by_xcd = [](int b, int n) {
-    const int xcd = b & 7, per = n >> 3, rem = n & 7;
-    return xcd * per + min(xcd, rem) + (b >> 3);
-  };
   const bool part = int(blockIdx.x) >= args.whole;
   int tile, s0 = 0, s1 = args.slabs, slot = 0;
   if (part) {
     slot = by_xcd(int(blockIdx.x) - args.whole, args.tail * args.parts);
-    const int q = slot / args.tail;
-    tile = args.whole + slot - q * args.tail;
-    s0 = q * args.per;
-    s1 = min(args.slabs, s0 + args.per);
+    part_place(slot, args.tail, args.per, args.slabs, tile, s0, s1);
+    tile += args.whole;
   } else {
     tile = by_xcd(int(blockIdx.x), args.whole);
   }

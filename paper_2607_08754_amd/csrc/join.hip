@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "block.hpp"
+#include "cut.hpp"
 #include "device.hpp"
 #include "layout.hpp"
 
@@ -30,7 +31,6 @@ namespace {
 void check(hipError_t e, const char *what) {
   if (e != hipSuccess) throw HipError(std::string(what) + ": " + hipGetErrorString(e));
 }
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ------------------------------------------------------------------ generator
 
@@ -343,7 +343,6 @@ __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
       const float r = norm_of<NV>(y, a, sh, turn);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        float ey[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float t = r * y.v[v][j];
