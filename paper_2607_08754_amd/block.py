@@ -25,6 +25,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 from typing import List, Optional, Tuple
 
 import torch
@@ -39,6 +40,8 @@ _DTYPE = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
 _ACT = {"silu": _lib.SILU, "gelu": _lib.GELU, "gelu_tanh": _lib.GELU_TANH}
 _NORM = {"rms": _lib.RMS, "layer": _lib.LAYER}
 _MAX_STRIDE = (1 << 22) - 8
+_MAX_NORM = 8192
+_MOST_P = (65535.5 - 2.0 ** -20) / 65536          # p counts in steps of 2^-16
 
 
 def _check_first(x: torch.Tensor, name: str) -> None:
@@ -51,7 +54,7 @@ def _check_first(x: torch.Tensor, name: str) -> None:
 
 
 def _check_like(t: torch.Tensor, shape, x: torch.Tensor, name: str) -> None:
-    if t.shape != shape or t.dtype != x.dtype or t.device != x.device:
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != x.dtype or t.device != x.device:
         raise ValueError(f"{name} must be a {x.dtype} {tuple(shape)} tensor on {x.device}")
 
 
@@ -158,7 +161,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     if act not in _ACT:
         raise ValueError(f"act must be one of {list(_ACT)}")
     dim = x.shape[-1]
-    if w_gate.dim() != 2 or w_gate.shape[0] < 1:
+    if not isinstance(w_gate, torch.Tensor) or w_gate.dim() != 2 or w_gate.shape[0] < 1:
         raise ValueError("w_gate must be a matrix of at least one row")
     inner = w_gate.shape[0]
     _check_dense(w_gate, (inner, dim), x, "w_gate")
@@ -261,12 +264,12 @@ def _gate_rows(gate: torch.Tensor, x: torch.Tensor) -> int:
 
 
 def _check_rng(p: float, rng, x: torch.Tensor) -> None:
-    if not 0.0 <= p < 1.0:
-        raise ValueError("p must be in [0, 1)")
+    if not 0.0 <= p <= _MOST_P:
+        raise ValueError("p must be in [0, 1), at most 1 - 2^-16 once rounded")
     if rng is None:
         if p > 0.0:
             raise ValueError("dropout needs rng")
-    elif rng.dtype != torch.int64 or rng.shape != (2,) or not rng.is_contiguous() or rng.device != x.device:
+    elif not isinstance(rng, torch.Tensor) or rng.dtype != torch.int64 or rng.shape != (2,) or not rng.is_contiguous() or rng.device != x.device:
         raise ValueError(f"rng must be an int64 tensor of two values on {x.device}")
 
 
@@ -274,6 +277,10 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
     if kind not in _NORM:
         raise ValueError(f"kind must be one of {list(_NORM)}")
     dim, gate = x.shape[-1], tensors[4]
+    if dim > _MAX_NORM:
+        raise ValueError(f"the last dimension must be at most {_MAX_NORM}")
+    if not (0.0 <= eps < math.inf and math.isfinite(alpha)):
+        raise ValueError("eps must be >= 0, eps and alpha finite")
     if f is not None:
         _check_like(f, x.shape, x, "f")
     for i in _VECTORS:
@@ -283,6 +290,8 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
     d = _lib.Join(rows, dim, _DTYPE[x.dtype], _NORM[kind], (_lib.JOIN_POST if post else 0) | (_lib.JOIN_PRE if pre else 0),
                   0, 0, 0, 0, float(eps), float(alpha), float(p), int(site))
     if gate is not None:
+        if not isinstance(gate, torch.Tensor) or gate.dim() < 1:
+            raise ValueError("gate must be a tensor")
         _check_like(gate, (*gate.shape[:-1], dim), x, "gate")
         d.gate_rows = _gate_rows(gate, x)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
@@ -380,6 +389,10 @@ class FeedForwardBlock(torch.nn.Module):
                  post: bool = False, scale: Optional[float] = None, p: float = 0.0, device=None,
                  dtype: torch.dtype = torch.bfloat16):
         super().__init__()
+        if act not in _ACT or kind not in _NORM:
+            raise ValueError(f"act must be one of {list(_ACT)}, kind one of {list(_NORM)}")
+        if not (1 <= dim <= _MAX_NORM and inner >= 1 and 0.0 <= p <= _MOST_P and dtype in _DTYPE):
+            raise ValueError(f"dim must be in [1, {_MAX_NORM}], inner at least 1, p in [0, 1), dtype float32 or bfloat16")
         kw = dict(device=device, dtype=dtype)
         self.act, self.kind, self.eps, self.p = act, kind, eps, p
 

@@ -111,6 +111,7 @@ slorr::JoinShape join_shape(const slorr_join_t *d) {
   s.ld_gate = d->ld_gate ? d->ld_gate : s.dim;
   if (s.ldx < s.dim || s.ldf < s.dim || s.ld_gate < s.dim) throw std::invalid_argument("a row stride is below dim");
   if (std::max({s.ldx, s.ldf, s.ld_gate}) > slorr::kMaxStride) throw std::domain_error("a row stride is beyond the limit");
+  if (s.rows > (int64_t(1) << 50) / std::max({s.ldx, s.ldf, s.ld_gate})) throw std::domain_error("rows times stride beyond the limit");
   s.gate_rows = d->gate_rows;
   if (!(d->eps >= 0.0f) || std::isinf(d->eps)) throw std::invalid_argument("eps must be >= 0 and finite");
   if (!std::isfinite(d->alpha)) throw std::invalid_argument("alpha must be finite");
