@@ -234,6 +234,73 @@ def run_sweep(which, kind, steps, warmup):
                       "sweep": rows}), flush=True)
 
 
+def run_blocks(kind, steps, warmup, depth=4, batch=16, seq=1024, p=0.1):
+    """The gated feed-forward blocks of each language-model set's shapes (random
+    weights, `depth` of them in a row, bf16, norms before and after, residual
+    dropout): a training step's forward and backward pass, the regularizer's
+    gradient on top of it (App. E.3), and one generated token; one JSON line."""
+    import torch
+    from paper_2607_08754_amd import FeedForwardBlock, Regularizer
+    from workloads import CONFIGS
+    dev = torch.device("cuda:0")
+
+    def timed(fn):
+        for _ in range(warmup):
+            fn()
+        torch.cuda.synchronize()
+        st, en = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        st.record()
+        for _ in range(steps):
+            fn()
+        en.record()
+        torch.cuda.synchronize()
+        return st.elapsed_time(en) / steps
+
+    rows = {}
+    for name in SWEEPS["llm"]:
+        inner, dim = next(s for s in CONFIGS[name].shapes if s[0] > s[1])
+        torch.manual_seed(0)
+        blocks = torch.nn.ModuleList(FeedForwardBlock(dim, inner, post=True, p=p, device=dev) for _ in range(depth))
+        reg = Regularizer([m for b in blocks for m in b.matrices()], kind=kind)
+        rng = torch.zeros(2, dtype=torch.int64, device=dev)
+        x = torch.randn(batch, seq, dim, dtype=torch.bfloat16, device=dev)
+        dy = torch.randn_like(x)
+
+        def forward(t):
+            for i, b in enumerate(blocks):
+                t = b(t, rng, site=i)
+            return t
+
+        def step():
+            blocks.zero_grad(set_to_none=True)
+            forward(x).backward(dy)
+            rng[1] += depth
+
+        def regularized():
+            step()
+            reg.accumulate_grad_(1e-4)
+
+        def token():
+            with torch.no_grad():
+                forward(one)
+
+        ms, ms_reg = timed(step), timed(regularized)
+        blocks.eval()
+        one = x[:1, :1].contiguous()
+        ms_token = timed(token)
+        flop = 18.0 * depth * batch * seq * dim * inner
+        rows[name] = {"dim": dim, "inner": inner, "ms_per_step": round(ms, 4), "product_tflops": round(flop / ms / 1e9, 1),
+                      "ms_per_step_with_slorr": round(ms_reg, 4), "slorr_share": round(1 - ms / ms_reg, 4),
+                      "ms_per_token": round(ms_token, 4)}
+        print(f"[blocks] {name}: {ms:.3f} ms/step, {ms_reg:.3f} with the regularizer, {ms_token:.4f} ms/token",
+              file=sys.stderr, flush=True)
+        del blocks, reg, x, dy
+        torch.cuda.empty_cache()
+    print(json.dumps({"metric": f"training step of {depth} gated feed-forward blocks with SLORR-{kind}", "unit": "ms/step",
+                      "steps": steps, "warmup": warmup, "dtype": "bf16", "data": "synthetic", "tokens": batch * seq,
+                      "blocks": rows}), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--gpus", type=int, default=1)
@@ -253,6 +320,9 @@ def main():
                     help="time every set of a sweep (App. D ViT configurations, App. F LLM shapes, "
                          "or the five configured sets) instead of the headline workload; prints one "
                          "JSON line")
+    ap.add_argument("--blocks", action="store_true",
+                    help="time training steps of the language-model sets' gated feed-forward blocks, with "
+                         "and without the regularizer, instead of the headline workload; prints one JSON line")
     args = ap.parse_args()
     if args.gpus != 1:
         print(f"bench.py measures one GPU only (got --gpus {args.gpus}); the hot path has no "
@@ -266,6 +336,10 @@ def main():
 
     if args.sweep:
         run_sweep(args.sweep, args.kind, max(1, min(args.steps, 20)), max(1, min(args.warmup, 3)))
+        return
+
+    if args.blocks:
+        run_blocks(args.kind, max(1, min(args.steps, 20)), max(1, min(args.warmup, 3)))
         return
 
     if args.calibrate_copy:
