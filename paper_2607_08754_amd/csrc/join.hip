@@ -720,9 +720,16 @@ __global__ __launch_bounds__(256) void k_dropout(int64_t n, uint32_t drop16, con
   }
 }
 
+// (nothing dropped)
 template <typename T>
 __global__ __launch_bounds__(256) void k_copy(int64_t n, const T *x, T *y) {
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) y[i] = x[i];
+  const int64_t pieces = (n + 7) >> 3;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
+    const int left = int(min(int64_t(8), n - i * 8));
+    float v[8];
+    widen<T>(get(x + i * 8, 0, left), v);
+    put(y + i * 8, 0, left, v);
+  }
 }
 
 float keep_factor(uint32_t drop) { return float(65536.0 / (65536.0 - double(drop))); }
@@ -794,7 +801,12 @@ void launch_backward(const JoinArgs &a, int mode, int64_t blocks, hipStream_t st
 
 JoinCut join_cut(const JoinShape &s) {
   JoinCut c;
-  const int64_t target = 4 * kCus;
+  // as many blocks as the CUs hold at once, by the kernels' registers: 16 waves per
+  // CU with bf16 rows of one piece per thread, else 8 (us with 4 blocks per CU
+  // whatever their size, and so: 65536 x 512 bf16 232, 123; 4096 x 4096 bf16 84, 65;
+  // 4096 x 6144 bf16 182, 151; 8192 x 4096 fp32 260, 224; 16384 x 1280 bf16 112, 109)
+  const int waves = s.dim <= 4096 && s.dtype == SLORR_BF16 ? 16 : 8;
+  const int64_t target = int64_t(kCus) * std::max(1, waves * 64 / join_threads(s.dim));
   const bool summed = s.gate_rows > 1 && s.gate_rows < s.rows;     // gate rows of several tokens each
   c.groups = summed ? s.gate_rows : 1;
   c.rows_per_group = s.rows / c.groups;
@@ -809,7 +821,8 @@ JoinCut join_cut(const JoinShape &s) {
     c.rows_per_part = c.rows_per_group;
     c.blocks = cdiv(c.groups, c.groups_per_block);
   } else {
-    c.parts = std::max<int64_t>(1, std::min(cdiv(target, c.groups), c.rows_per_group));
+    // (parts of at least 4 rows: each leaves partial rows to write and to add)
+    c.parts = std::max<int64_t>(1, std::min(cdiv(target, c.groups), cdiv(c.rows_per_group, 4)));
     c.rows_per_part = std::max<int64_t>(1, cdiv(c.rows_per_group, c.parts));
     c.parts = std::max<int64_t>(1, cdiv(c.rows_per_group, c.rows_per_part));
     c.groups_per_block = 1;
@@ -829,9 +842,12 @@ void enqueue_join_forward(const JoinShape &s, const slorr_join_tensors_t &t, con
   JoinArgs a = join_args(s, t, rng);
   a.y = y;
   a.z = z;
-  // as many blocks as the CUs hold at once (16 waves each), each a run of rows
+  // as many blocks as the CUs hold at once, each a run of rows: 16 waves per CU, 24
+  // where the registers allow it (16384 x 1280 bf16: 51.7 us with 16, 45.2 with 24;
+  // the others are no faster or slower, 4096 x 6144 bf16 48.5 and 54.6)
   const int threads = join_threads(s.dim);
-  a.per_block = std::max<int64_t>(1, cdiv(s.rows, kCus * (16 * 64 / threads)));
+  const int waves = s.dim <= 4096 && s.dtype == SLORR_BF16 && !a.b1 && !a.b2 ? 24 : 16;
+  a.per_block = std::max<int64_t>(1, cdiv(s.rows, kCus * (waves * 64 / threads)));
   const uint32_t grid = uint32_t(cdiv(s.rows, a.per_block));
   if (s.dtype == SLORR_BF16) launch_forward<bf16_t>(a, grid, threads, st);
   else launch_forward<float>(a, grid, threads, st);
@@ -862,13 +878,13 @@ void enqueue_join_backward(const JoinShape &s, const slorr_join_tensors_t &t, co
       q.from[q.kinds++] = i;
     }
   const bool each = a.gate && a.gate_run == 1 && s.gate_rows == s.rows;
-  // the gate's sums are joined afterwards where a gate row's tokens are spread
-  // over blocks, and where there is no token to write them
-  const bool joined = g.gate && (!s.rows || (!each && (c.parts > 1 || s.dim > 4096)));
+  const int mode = each ? kEachRow : a.gate && c.groups > 1 && c.parts == 1 && s.dim <= 4096 ? kGroups : kOneGate;
+  // kOneGate's blocks leave parts of the gate's sums, to be added afterwards (with no
+  // token at all: zeros)
+  const bool joined = g.gate && (!s.rows || mode == kOneGate);
   a.part = q.kinds ? w : nullptr;
   a.gpart = joined ? w + 5 * n : nullptr;
   if (s.rows) {
-    const int mode = each ? kEachRow : a.gate && c.groups > 1 && c.parts == 1 && s.dim <= 4096 ? kGroups : kOneGate;
     if (s.dtype == SLORR_BF16) launch_backward<bf16_t>(a, mode, c.blocks, st);
     else launch_backward<float>(a, mode, c.blocks, st);
   }
@@ -899,8 +915,7 @@ void enqueue_join_backward(const JoinShape &s, const slorr_join_tensors_t &t, co
 void enqueue_dropout(int64_t n, int32_t dtype, uint32_t drop, const int64_t *rng, int64_t site, const void *x,
                      void *y, hipStream_t st) {
   if (!n || (!drop && x == y)) return;
-  const int64_t pieces = drop ? cdiv(n, 8) : n;
-  const dim3 grid(uint32_t(std::min<int64_t>(cdiv(pieces, 256), 32 * kCus))), block(256);
+  const dim3 grid(uint32_t(std::min<int64_t>(cdiv(cdiv(n, 8), 256), 32 * kCus))), block(256);
   if (dtype == SLORR_BF16) {
     const bf16_t *p = static_cast<const bf16_t *>(x);
     bf16_t *q = static_cast<bf16_t *>(y);
