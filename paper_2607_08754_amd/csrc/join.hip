@@ -34,6 +34,9 @@ void check(hipError_t e, const char *what) {
 
 // ------------------------------------------------------------------ generator
 
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);       // (the table of a ^ b ^ c)
+}
 // One block of Philox4x32-10: ten rounds of two 32 x 32 -> 64 products.
 __device__ __forceinline__ void philox(uint64_t index, uint64_t offset, uint64_t key, uint32_t (&c)[4]) {
   c[0] = uint32_t(index);
@@ -44,9 +47,9 @@ __device__ __forceinline__ void philox(uint64_t index, uint64_t offset, uint64_t
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = uint64_t(c[0]) * 0xD2511F53u, b = uint64_t(c[2]) * 0xCD9E8D57u;
-    c[0] = uint32_t(b >> 32) ^ c[1] ^ k0;
+    c[0] = xor3(uint32_t(b >> 32), c[1], k0);
     c[1] = uint32_t(b);
-    c[2] = uint32_t(a >> 32) ^ c[3] ^ k1;
+    c[2] = xor3(uint32_t(a >> 32), c[3], k1);
     c[3] = uint32_t(a);
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -63,11 +66,15 @@ __device__ __forceinline__ Rng load_rng(const int64_t *rng, int64_t site) {
 // Eight elements' factors, k where element e + j is kept and 0 elsewhere. drop16
 // is the threshold in the upper half of a word: the upper 16-bit number of a word
 // is compared in place, the lower one shifted up. A run of eight that does not
-// start at a multiple of 8 takes two generator blocks.
-__device__ __forceinline__ void keep8(int64_t e, const Rng &r, uint32_t drop16, float k, float (&m)[8]) {
+// start at a multiple of 8 takes two generator blocks; s, the element's place in
+// its block, is the same over a wave.
+template <bool NOW>
+__device__ __forceinline__ void keep8(int64_t e, int s, Rng r, uint32_t drop16, float k, float (&m)[8]) {
+  // NOW: the rounds' keys are formed here. Held over the loop over rows they fill the
+  // scalar registers and are fetched from lanes of vector ones, 29 instructions a row.
+  if constexpr (NOW) asm volatile("" : "+s"(r.key));
   uint32_t c[4];
   philox(uint64_t(e) >> 3, r.offset, r.key, c);
-  const int s = int(e & 7);
   if (s) {
     uint32_t n[4];
     philox((uint64_t(e) >> 3) + 1, r.offset, r.key, n);
@@ -129,6 +136,25 @@ __device__ __forceinline__ void put(T *row, int c, int dim, const float (&v)[8])
   }
 }
 
+// A row's piece. WHOLE: rows of whole pieces (dim a multiple of 8), without the code
+// for a row's last columns.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ Raw<T> piece_of(const T *row, int c, int dim) {
+  if constexpr (!WHOLE) return get(row, c, dim);
+  Raw<T> r = {};
+  if (c < dim) {
+    const SLORR_GLOBAL u32x4_any *p = (const SLORR_GLOBAL u32x4_any *)(row + c);
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) r.q[i] = p[i];
+  }
+  return r;
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void put_piece(T *row, int c, int dim, const float (&v)[8]) {
+  if constexpr (!WHOLE) put(row, c, dim, v);
+  else if (c < dim) put(row + c, 0, 8, v);
+}
+
 // NV pieces of 8 columns per thread, as fp32.
 template <int NV>
 struct Row {
@@ -136,10 +162,10 @@ struct Row {
 };
 __device__ __forceinline__ int column(int v) { return (v * int(blockDim.x) + int(threadIdx.x)) * 8; }
 
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void vector8(const void *p, int c, int dim, float none, float (&o)[8]) {
   if (p) {
-    widen<T>(get(static_cast<const T *>(p), c, dim), o);
+    widen<T>(piece_of<WHOLE>(static_cast<const T *>(p), c, dim), o);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = none;
@@ -241,9 +267,11 @@ __device__ __forceinline__ float norm_of(Row<NV> &t, const JoinArgs &a, RowSums 
 }
 
 // The factors of a row's piece: k D.
+template <bool NOW>
 __device__ __forceinline__ void factors(const JoinArgs &a, const Rng &rng, int64_t row, int c, float k, float (&m)[8]) {
   if (a.drop16) {
-    keep8(row * a.dim + c, rng, a.drop16, k, m);
+    const int64_t base = row * a.dim;
+    keep8<NOW>(base + c, int(base) & 7, rng, a.drop16, k, m);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) m[j] = k;
@@ -258,23 +286,23 @@ __device__ __forceinline__ const void *unmoved(const void *p) {
 }
 
 // s g w1 and s g b1 of a piece for a gate row (null: 1).
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void product8(const JoinArgs &a, const T *gate, int v, float (&sgw)[8], float (&sgb)[8]) {
   float w[8], b[8], s[8], g[8];
-  vector8<T>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
-  vector8<T>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
-  vector8<T>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
-  vector8<T>(unmoved(gate), column(v), a.dim, 1.0f, g);
+  vector8<T, WHOLE>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
+  vector8<T, WHOLE>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
+  vector8<T, WHOLE>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
+  vector8<T, WHOLE>(unmoved(gate), column(v), a.dim, 1.0f, g);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     sgw[j] = s[j] * g[j] * w[j];
     sgb[j] = s[j] * g[j] * b[j];
   }
 }
-template <typename T, int NV>
+template <typename T, bool WHOLE, int NV>
 __device__ __forceinline__ void products(const JoinArgs &a, const T *gate, Row<NV> &sgw, Row<NV> &sgb) {
 #pragma unroll
-  for (int v = 0; v < NV; ++v) product8<T>(a, gate, v, sgw.v[v], sgb.v[v]);
+  for (int v = 0; v < NV; ++v) product8<T, WHOLE>(a, gate, v, sgw.v[v], sgb.v[v]);
 }
 
 // A block takes a run of rows, each thread NV pieces of 8 columns of a row; the
@@ -282,7 +310,7 @@ __device__ __forceinline__ void products(const JoinArgs &a, const T *gate, Row<N
 // products are formed once per gate row. What bounds these kernels is the
 // instructions of a row (the generator's share: 20 32 x 32 products and 60 others
 // per 8 elements) as much as HBM.
-template <typename T, int NV, bool BIAS>
+template <typename T, int NV, bool BIAS, bool WHOLE>
 __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
   __shared__ RowSums sh;
   row_sums_init(sh);
@@ -293,26 +321,26 @@ __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      nx[v] = get(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
-      if (a.f) nf[v] = get(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
+      nx[v] = piece_of<WHOLE>(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
+      if (a.f) nf[v] = piece_of<WHOLE>(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
     }
   };
   if (r0 < r1) fetch(r0);
   Row<NV> sgw, sgb, w2, b2;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    vector8<T>(a.w2, column(v), a.dim, 1.0f, w2.v[v]);
-    if constexpr (BIAS) vector8<T>(a.b2, column(v), a.dim, 0.0f, b2.v[v]);
+    vector8<T, WHOLE>(a.w2, column(v), a.dim, 1.0f, w2.v[v]);
+    if constexpr (BIAS) vector8<T, WHOLE>(a.b2, column(v), a.dim, 0.0f, b2.v[v]);
   }
   int64_t gate_row = a.gate ? r0 / a.gate_run : 0, gate_end = a.gate ? (gate_row + 1) * a.gate_run : a.rows;
   if (a.f && r0 < r1)
-    products<T>(a, a.gate ? static_cast<const T *>(a.gate) + gate_row * a.ldg : nullptr, sgw, sgb);
+    products<T, WHOLE>(a, a.gate ? static_cast<const T *>(a.gate) + gate_row * a.ldg : nullptr, sgw, sgb);
 #pragma unroll 1
   for (int64_t row = r0; row < r1; ++row) {
     if (a.f && row == gate_end) {
       ++gate_row;
       gate_end += a.gate_run;
-      products<T>(a, static_cast<const T *>(a.gate) + gate_row * a.ldg, sgw, sgb);
+      products<T, WHOLE>(a, static_cast<const T *>(a.gate) + gate_row * a.ldg, sgw, sgb);
     }
     Row<NV> y, u;
 #pragma unroll
@@ -326,7 +354,7 @@ __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float m[8];
-        factors(a, rng, row, column(v), a.k, m);
+        factors<NV == 1>(a, rng, row, column(v), a.k, m);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float t = r * u.v[v][j];
@@ -336,7 +364,7 @@ __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
     }
     if (a.y) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) put(static_cast<T *>(a.y) + row * a.dim, column(v), a.dim, y.v[v]);
+      for (int v = 0; v < NV; ++v) put_piece<WHOLE>(static_cast<T *>(a.y) + row * a.dim, column(v), a.dim, y.v[v]);
     }
     if (a.pre) {
       // (columns past dim hold zeros: the vectors and rows end there)
@@ -348,7 +376,7 @@ __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
           const float t = r * y.v[v][j];
           y.v[v][j] = BIAS ? fmaf(t, w2.v[v][j], b2.v[v][j]) : t * w2.v[v][j];
         }
-        put(static_cast<T *>(a.z) + row * a.dim, column(v), a.dim, y.v[v]);
+        put_piece<WHOLE>(static_cast<T *>(a.z) + row * a.dim, column(v), a.dim, y.v[v]);
       }
     }
   }
@@ -370,7 +398,7 @@ enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2 };
 //
 // A row has three block sums one after the other (RMS; LAYER five): the next
 // row is loaded before them, and the y norm's two sums share one.
-template <typename T, int NV, int MODE, bool BIAS>
+template <typename T, int NV, int MODE, bool BIAS, bool WHOLE>
 __global__ __launch_bounds__(512, NV == 1 && MODE == kOneGate && !BIAS && sizeof(T) == 2 ? 4 : 2)
 void k_join_bwd(JoinArgs a) {
   __shared__ RowSums sh;
@@ -426,21 +454,21 @@ void k_join_bwd(JoinArgs a) {
   auto fetch_dy = [&](int64_t row) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if (a.dy) nd[v] = get(static_cast<const T *>(a.dy) + row * a.dim, column(v), a.dim);
+      if (a.dy) nd[v] = piece_of<WHOLE>(static_cast<const T *>(a.dy) + row * a.dim, column(v), a.dim);
   };
   auto fetch_gate = [&](int64_t gr) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if constexpr (MODE != kOneGate) ng[v] = get(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
+      if constexpr (MODE != kOneGate) ng[v] = piece_of<WHOLE>(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
   };
   auto fetch = [&](int64_t row, int64_t gr) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      nx[v] = get(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
-      if (a.f) nf[v] = get(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
-      if (a.dz) nz[v] = get(static_cast<const T *>(a.dz) + row * a.dim, column(v), a.dim);
+      nx[v] = piece_of<WHOLE>(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
+      if (a.f) nf[v] = piece_of<WHOLE>(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
+      if (a.dz) nz[v] = piece_of<WHOLE>(static_cast<const T *>(a.dz) + row * a.dim, column(v), a.dim);
       if constexpr (!kAhead && MODE != kOneGate)
-        ng[v] = get(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
+        ng[v] = piece_of<WHOLE>(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
     }
     if (kAhead) {
       fetch_dy(row);
@@ -449,13 +477,13 @@ void k_join_bwd(JoinArgs a) {
   };
   Row<NV> sgw, sgb, w2;
   if (kAhead && r0 < r1) fetch(r0, gate_row);
-  if (kAhead && a.f) products<T>(a, gate0, sgw, sgb);
+  if (kAhead && a.f) products<T, WHOLE>(a, gate0, sgw, sgb);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) vector8<T>(a.w2, column(v), a.dim, 1.0f, w2.v[v]);
+  for (int v = 0; v < NV; ++v) vector8<T, WHOLE>(a.w2, column(v), a.dim, 1.0f, w2.v[v]);
   auto piece = [&](int v) {
     if (!kAhead) {
       __builtin_amdgcn_sched_barrier(0);
-      product8<T>(a, gate0, v, sgw.v[v], sgb.v[v]);
+      product8<T, WHOLE>(a, gate0, v, sgw.v[v], sgb.v[v]);
     }
   };
 
@@ -505,7 +533,7 @@ void k_join_bwd(JoinArgs a) {
       }
       if (kAhead) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) factors(a, rng, row, column(v), 1.0f, m.v[v]);
+        for (int v = 0; v < NV; ++v) factors<NV == 1>(a, rng, row, column(v), 1.0f, m.v[v]);
       }
     }
     if (a.dz) {
@@ -514,7 +542,7 @@ void k_join_bwd(JoinArgs a) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
           piece(v);
-          if (!kAhead) factors(a, rng, row, column(v), 1.0f, m.v[v]);
+          if (!kAhead) factors<NV == 1>(a, rng, row, column(v), 1.0f, m.v[v]);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float km = MODE == kOneGate ? a.k * m.v[v][j] : a.k * m.v[v][j] * g.v[v][j];
@@ -566,14 +594,14 @@ void k_join_bwd(JoinArgs a) {
     if (!kAhead && !a.dz) take_dy();
     if (a.dx) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) put(static_cast<T *>(a.dx) + row * a.dim, column(v), a.dim, d.v[v]);
+      for (int v = 0; v < NV; ++v) put_piece<WHOLE>(static_cast<T *>(a.dx) + row * a.dim, column(v), a.dim, d.v[v]);
     }
     if (!a.f) continue;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float dg[8], du[8];
       piece(v);
-      if (!kAhead) factors(a, rng, row, column(v), 1.0f, m.v[v]);
+      if (!kAhead) factors<NV == 1>(a, rng, row, column(v), 1.0f, m.v[v]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         d.v[v][j] *= m.v[v][j];                                  // dY D
@@ -593,7 +621,7 @@ void k_join_bwd(JoinArgs a) {
       for (int j = 0; j < 8; ++j) d.v[v][j] *= a.k * sgw.v[v][j];
       if constexpr (MODE != kOneGate) {
         if (turns) {
-          if (a.dgate) put(static_cast<T *>(a.dgate) + this_gate * a.dim, column(v), a.dim, dg);
+          if (a.dgate) put_piece<WHOLE>(static_cast<T *>(a.dgate) + this_gate * a.dim, column(v), a.dim, dg);
           if constexpr (MODE == kGroups) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) sg.v[v][j] = 0.0f;
@@ -619,7 +647,7 @@ void k_join_bwd(JoinArgs a) {
           for (int j = 0; j < 8; ++j) d.v[v][j] = rf * fmaf(-u.v[v][j], mt, d.v[v][j] - mean);
       }
 #pragma unroll
-      for (int v = 0; v < NV; ++v) put(static_cast<T *>(a.df) + row * a.dim, column(v), a.dim, d.v[v]);
+      for (int v = 0; v < NV; ++v) put_piece<WHOLE>(static_cast<T *>(a.df) + row * a.dim, column(v), a.dim, d.v[v]);
     }
   }
 
@@ -634,10 +662,10 @@ void k_join_bwd(JoinArgs a) {
       take(2, v, P.v[v]);
       take(3, v, sw2.v[v]);
     }
-    vector8<T>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
-    vector8<T>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
-    vector8<T>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
-    vector8<T>(unmoved(gate0), column(v), a.dim, 1.0f, g);
+    vector8<T, WHOLE>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
+    vector8<T, WHOLE>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
+    vector8<T, WHOLE>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
+    vector8<T, WHOLE>(unmoved(gate0), column(v), a.dim, 1.0f, g);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float q = a.k * (BIAS ? fmaf(w[j], P.v[v][j], b[j] * Q.v[v][j]) : w[j] * P.v[v][j]);
@@ -670,7 +698,7 @@ struct SumArgs {
 };
 template <typename T>
 __global__ __launch_bounds__(1024) void k_join_sum(SumArgs a) {
-  __shared__ float sh[16][64];
+  __shared__ __attribute__((aligned(16))) float sh[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   const int item = blockIdx.y;
   const float *p;
@@ -686,15 +714,23 @@ __global__ __launch_bounds__(1024) void k_join_sum(SumArgs a) {
     n = a.parts;
     out = static_cast<T *>(a.dgate) + g * a.dim;
   }
-  float s[4] = {};
-  if (c < a.dim) {
-    int64_t i = wave;
-    for (; i + 48 < n; i += 64)
+  // a wave takes four rows at once, 16 bytes of 16 lanes each; four such loads ahead
+  const int c4 = blockIdx.x * 64 + (lane & 15) * 4;
+  float4v s[4] = {};
+  if (c4 < a.ldp) {
+    int64_t i = wave * 4 + (lane >> 4);
+    for (; i + 192 < n; i += 256)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) s[q] += p[(i + 16 * q) * a.ldp + c];
-    for (; i < n; i += 16) s[0] += p[i * a.ldp + c];
+      for (int q = 0; q < 4; ++q) s[q] += *reinterpret_cast<const float4v *>(p + (i + 64 * q) * a.ldp + c4);
+    for (; i < n; i += 64) s[0] += *reinterpret_cast<const float4v *>(p + i * a.ldp + c4);
   }
-  sh[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+  s[0] = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    s[0][j] += __shfl_xor(s[0][j], 16);
+    s[0][j] += __shfl_xor(s[0][j], 32);
+  }
+  if (lane < 16) *reinterpret_cast<float4v *>(&sh[wave][lane * 4]) = s[0];
   __syncthreads();
   if (wave == 0 && c < a.dim) {
     float t = 0.0f;
@@ -712,7 +748,7 @@ __global__ __launch_bounds__(256) void k_dropout(int64_t n, uint32_t drop16, con
     const int left = int(min(int64_t(8), n - i * 8));
     const Raw<T> r = get(x + i * 8, 0, left);
     float v[8], m[8];
-    keep8(i * 8, rng, drop16, keep, m);
+    keep8<false>(i * 8, 0, rng, drop16, keep, m);
     widen<T>(r, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = m[j] != 0.0f ? v[j] * keep : 0.0f;
@@ -766,24 +802,33 @@ JoinArgs join_args(const JoinShape &s, const slorr_join_tensors_t &t, const int6
   return a;
 }
 
+template <typename T, int NV, bool BIAS>
+void launch_forward_as(const JoinArgs &a, dim3 grid, dim3 block, hipStream_t st) {
+  if (a.dim % 8) hipLaunchKernelGGL((k_join_fwd<T, NV, BIAS, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_join_fwd<T, NV, BIAS, true>), grid, block, 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+}
 template <typename T>
-void launch_forward(const JoinArgs &a, uint32_t grid, int threads, hipStream_t st) {
+void launch_forward(const JoinArgs &a, uint32_t blocks, int threads, hipStream_t st) {
+  const dim3 grid(blocks), block(threads);
   const bool bias = a.b1 || a.b2;
-  if (a.dim > 4096) {
-    if (bias) hipLaunchKernelGGL((k_join_fwd<T, 2, true>), dim3(grid), dim3(threads), 0, st, a);
-    else hipLaunchKernelGGL((k_join_fwd<T, 2, false>), dim3(grid), dim3(threads), 0, st, a);
-  } else {
-    if (bias) hipLaunchKernelGGL((k_join_fwd<T, 1, true>), dim3(grid), dim3(threads), 0, st, a);
-    else hipLaunchKernelGGL((k_join_fwd<T, 1, false>), dim3(grid), dim3(threads), 0, st, a);
-  }
+  if (a.dim > 4096 && bias) launch_forward_as<T, 2, true>(a, grid, block, st);
+  else if (a.dim > 4096) launch_forward_as<T, 2, false>(a, grid, block, st);
+  else if (bias) launch_forward_as<T, 1, true>(a, grid, block, st);
+  else launch_forward_as<T, 1, false>(a, grid, block, st);
 }
 
+template <typename T, int NV, int MODE, bool BIAS>
+void launch_backward_in(const JoinArgs &a, dim3 grid, dim3 block, hipStream_t st) {
+  if (a.dim % 8) hipLaunchKernelGGL((k_join_bwd<T, NV, MODE, BIAS, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_join_bwd<T, NV, MODE, BIAS, true>), grid, block, 0, st, a);
+  check(hipGetLastError(), "kernel launch");
+}
 template <typename T, int NV, int MODE>
 void launch_backward_as(const JoinArgs &a, int64_t blocks, hipStream_t st) {
   const dim3 grid{uint32_t(blocks)}, block(join_threads(a.dim));
-  if (a.b1 || a.b2) hipLaunchKernelGGL((k_join_bwd<T, NV, MODE, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_join_bwd<T, NV, MODE, false>), grid, block, 0, st, a);
-  check(hipGetLastError(), "kernel launch");
+  if (a.b1 || a.b2) launch_backward_in<T, NV, MODE, true>(a, grid, block, st);
+  else launch_backward_in<T, NV, MODE, false>(a, grid, block, st);
 }
 template <typename T, int NV>
 void launch_backward_of(const JoinArgs &a, int mode, int64_t blocks, hipStream_t st) {
@@ -851,7 +896,6 @@ void enqueue_join_forward(const JoinShape &s, const slorr_join_tensors_t &t, con
   const uint32_t grid = uint32_t(cdiv(s.rows, a.per_block));
   if (s.dtype == SLORR_BF16) launch_forward<bf16_t>(a, grid, threads, st);
   else launch_forward<float>(a, grid, threads, st);
-  check(hipGetLastError(), "kernel launch");
 }
 
 void enqueue_join_backward(const JoinShape &s, const slorr_join_tensors_t &t, const int64_t *rng, const void *dy,
