@@ -25,7 +25,7 @@ enum FfnEpi { kStore = 0, kAct = 1, kActBack = 2 };
 // there is), and for its start and end (kActBack, which loads and stores five
 // values per sum: back). From 16384 x 1536 x 6144 in bf16, us of a round of each:
 // the weight gradients' 256 slabs 467 and 276, y's 96 slabs 184 and 119, dh's 24
-// slabs 87 and 47 (a round of the first is twice the work of the other's).
+// slabs 81 and 49 (a round of the first is twice the work of the other's).
 // Not kept: 256 x 128 with three LDS stages (1.15 us a slab: two 128-tiles, with
 // longer ends), 128 x 128 with four stages and one block per CU (0.6 us a slab:
 // 16384 x 1280 x 3456 backward 1017 -> 1303 us where it ran, 100 x 1536 x 6144
@@ -34,8 +34,8 @@ struct TileKind {
   int bm, bn, slots;
   double slab, alone, ends, back;
 };
-constexpr TileKind kTiles[] = {{256, 256, kCus, 1.77, 1.77, 13, 44},
-                               {128, 128, 2 * kCus, 1.15, 0.75, 4, 18}};
+constexpr TileKind kTiles[] = {{256, 256, kCus, 1.77, 1.77, 13, 38},
+                               {128, 128, 2 * kCus, 1.15, 0.75, 4, 20}};
 constexpr double kPartByte = 2 / 4.5e6;                   // a part's sums, written and read once at 4.5 TB/s
 constexpr double kTailLaunch = 5;
 

@@ -46,13 +46,13 @@ template <bool F32>
 __device__ __forceinline__ float sigmoid(float a) {
   return __builtin_amdgcn_rcpf(1.0f + (F32 ? expf(-a) : __expf(-a)));
 }
-template <bool F32>
-__device__ __forceinline__ void act_and_slope(int act, float a, float &f, float &s) {
-  if (act == SLORR_SILU) {
+template <bool F32, int ACT>
+__device__ __forceinline__ void act_and_slope(float a, float &f, float &s) {
+  if constexpr (ACT == SLORR_SILU) {
     const float g = sigmoid<F32>(a);
     f = a * g;
     s = g * (1.0f + a * (1.0f - g));
-  } else if (act == SLORR_GELU) {
+  } else if constexpr (ACT == SLORR_GELU) {
     const float c = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
     f = a * c;
     s = c + a * (F32 ? expf(-0.5f * a * a) : __expf(-0.5f * a * a)) * 0.39894228040143268f;
@@ -62,6 +62,14 @@ __device__ __forceinline__ void act_and_slope(int act, float a, float &f, float 
     f = a * g;
     s = g + f * (1.0f - g) * k * (1.0f + 3.0f * q);
   }
+}
+// The activation chosen once for a run of values: a choice per value keeps the
+// values' chains of dependent instructions from overlapping.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F run) {
+  if (act == SLORR_SILU) run(std::integral_constant<int, SLORR_SILU>{});
+  else if (act == SLORR_GELU) run(std::integral_constant<int, SLORR_GELU>{});
+  else run(std::integral_constant<int, SLORR_GELU_TANH>{});
 }
 
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
@@ -170,6 +178,16 @@ struct KeptRaw {
     } else {
       q[0] = gload16(static_cast<const uint16_t *>(k.v) + k.at(row, col));
       e = *(const SLORR_GLOBAL uint8_t *)(k.e + k.exp_at(row, col));
+    }
+  }
+  // values 4 i to 4 i + 3 (bf16 tensors)
+  __device__ __forceinline__ void half(int i, float4v &v) const {
+    if (e == 255) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = to_f(bf16_t(q[0][2 * i + (j >> 1)] >> (16 * (j & 1))));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = ldexpf(float(int16_t(q[0][2 * i + (j >> 1)] >> (16 * (j & 1)))), int(e) - 141);
     }
   }
   __device__ __forceinline__ void values(float (&v)[8]) const {
@@ -312,28 +330,60 @@ __device__ __forceinline__ void finish(const FfnArgs &args, const FfnProb &pr, i
       store_kept<F32>(args.a, row, col, v);
       store_kept<F32>(args.b, row, col, b);
     }
+    with_act(args.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float f, sl;
-      act_and_slope<F32>(args.act, v[j], f, sl);
-      h[j] = f * b[j];
-    }
+      for (int j = 0; j < 8; ++j) {
+        float f, sl;
+        act_and_slope<F32, decltype(act)::value>(v[j], f, sl);
+        h[j] = f * b[j];
+      }
+    });
     store_planes<F32>(args.h + at * 2, args.plane, h);
   } else {
-    float a[8], da[8], db[8];
-    kept.a.values(a);
-    kept.b.values(b);
+    with_act(args.act, [&](auto act) {
+      auto one = [&](float a, float bj, float vj, float &hj, float &da, float &db) {
+        float f, sl;
+        act_and_slope<F32, decltype(act)::value>(a, f, sl);
+        hj = f * bj;
+        db = vj * f;
+        da = vj * bj * sl;
+      };
+      if constexpr (F32) {
+        float a[8], da[8], db[8];
+        kept.a.values(a);
+        kept.b.values(b);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float f, sl;
-      act_and_slope<F32>(args.act, a[j], f, sl);
-      h[j] = f * b[j];
-      db[j] = v[j] * f;
-      da[j] = v[j] * b[j] * sl;
-    }
-    store_planes<F32>(args.h + at * 2, args.plane, h);
-    store_planes<F32>(args.da + at * 2, args.plane, da);
-    store_planes<F32>(args.db + at * 2, args.plane, db);
+        for (int j = 0; j < 8; ++j) one(a[j], b[j], v[j], h[j], da[j], db[j]);
+        store_planes<true>(args.h + at * 2, args.plane, h);
+        store_planes<true>(args.da + at * 2, args.plane, da);
+        store_planes<true>(args.db + at * 2, args.plane, db);
+      } else {
+        // four values at a time, rounded before the next four: the registers hold the
+        // sums and the next block's a and b as well
+        bf16x4 o[3][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float4v r[3], a4, b4;
+          kept.a.half(i, a4);
+          kept.b.half(i, b4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float x, y, z;
+            one(a4[j], b4[j], v[4 * i + j], x, y, z);
+            r[0][j] = x;
+            r[1][j] = y;
+            r[2][j] = z;
+          }
+#pragma unroll
+          for (int q = 0; q < 3; ++q) o[q][i] = __builtin_convertvector(r[q], bf16x4);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        char *const to[3] = {args.h, args.da, args.db};
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+          *reinterpret_cast<bf16x8 *>(to[q] + at * 2) = __builtin_shufflevector(o[q][0], o[q][1], 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    });
   }
 }
 
@@ -443,18 +493,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
   // no registers for more)
   constexpr int PC = EPI == kAct ? 4 : 8;                 // 8-column pieces per row
   constexpr int kTasks = 32 * PC / 64;
-  constexpr int kAhead = F32 ? 0 : 1;
-  KeptPair<F32> kept[EPI == kActBack ? kAhead + 1 : 1][EPI == kActBack ? kTasks : 1];
-  auto kept_load = [&](int i) {
-    if constexpr (EPI == kActBack) {
-#pragma unroll
-      for (int t = 0; t < kTasks; ++t) {
-        const int task = lane + 64 * t;
-        kept[kAhead ? i & 1 : 0][t].load(args, pr.m, m0 + wm * S::WTM + i * 32 + task / PC, n0 + wn * 64 + (task % PC) * 8);
-      }
-    }
+  constexpr bool kAhead = EPI == kActBack && !F32;
+  KeptPair<F32> kept[kAhead ? kTasks : 1];
+  auto kept_load = [&](int i, int t) {
+    const int task = lane + 64 * t;
+    kept[t].load(args, pr.m, m0 + wm * S::WTM + i * 32 + task / PC, n0 + wn * 64 + (task % PC) * 8);
   };
-  if (kAhead && !part) kept_load(0);
+  if constexpr (kAhead) {
+    if (!part) {
+#pragma unroll
+      for (int t = 0; t < kTasks; ++t) kept_load(0, t);
+    }
+  }
 
 #pragma unroll
   for (int q = 0; q < NS - 1; ++q)
@@ -511,7 +561,6 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
             float4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
     __builtin_amdgcn_wave_barrier();
     const int row0 = wm * S::WTM + i * 32;
-    if (kAhead && i + 1 < FM && !part) kept_load(i + 1);
     constexpr int kCopies = F32 && EPI != kStore ? 1 : kTasks;   // fp32 activations are long code
 #pragma unroll kCopies
     for (int t = 0; t < kTasks; ++t) {
@@ -531,12 +580,12 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_ffn(FfnArgs args) {
         if constexpr (EPI == kAct) store_whole<true>(args.part, at + 32, b);
       } else {
         KeptPair<F32> k;
-        if constexpr (EPI == kActBack) {
-          // (the rolled loop of fp32 tensors cannot name its registers)
-          if constexpr (kCopies == 1) k.load(args, pr.m, m0 + row0 + rl, n0 + wn * 64 + cl);
-          else k = kept[kAhead ? i & 1 : 0][t];
-        }
+        if constexpr (kAhead) k = kept[t];
+        else if constexpr (EPI == kActBack) k.load(args, pr.m, m0 + row0 + rl, n0 + wn * 64 + cl);
         finish<EPI, F32>(args, pr, m0 + row0 + rl, n0 + wn * (EPI == kAct ? 32 : 64) + cl, v, b, k);
+        if constexpr (kAhead) {
+          if (i + 1 < FM) kept_load(i + 1, t);
+        }
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -666,16 +715,19 @@ __global__ __launch_bounds__(TF > 2 ? 512 : 1024) void k_few(FewArgs a) {
     const int token = 16 * t + r, n = n0 + 4 * (lane >> 4);
     if (token >= a.tokens) continue;
     T *o = static_cast<T *>(a.out) + token * a.ldo + n;
+    if constexpr (DUAL) {
+      with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float v = s[0][j];
-      if constexpr (DUAL) {
-        float f, slope;
-        act_and_slope<F32>(a.act, v, f, slope);
-        v = f * s[NF - 1][j];
-      }
-      if (n + j < a.n) o[j] = from_f<T>(v);
+        for (int j = 0; j < 4; ++j) {
+          float f, slope;
+          act_and_slope<F32, decltype(act)::value>(s[0][j], f, slope);
+          s[0][j] = f * s[NF - 1][j];
+        }
+      });
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n + j < a.n) o[j] = from_f<T>(s[0][j]);
   }
 }
 

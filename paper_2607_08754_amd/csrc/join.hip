@@ -307,9 +307,11 @@ __device__ __forceinline__ void products(const JoinArgs &a, const T *gate, Row<N
 
 // A block takes a run of rows, each thread NV pieces of 8 columns of a row; the
 // next row's loads are issued before the current row's sums, and the vectors'
-// products are formed once per gate row. What bounds these kernels is the
-// instructions of a row (the generator's share: 20 32 x 32 products and 60 others
-// per 8 elements) as much as HBM.
+// products are formed once per gate row. WHOLE: rows of whole pieces; the code for
+// a row's end, which is there for every tensor, costs 16384 x 1280 bf16 3 of 35 us
+// (backward 23 of 92) even where no row has one. HBM bounds the kernel (168 MB in 28 us, 6.0
+// TB/s) up to the generator, whose 20 32 x 32 products and 40 other instructions
+// per 8 elements add 3.7 us.
 template <typename T, int NV, bool BIAS, bool WHOLE>
 __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
   __shared__ RowSums sh;
@@ -888,8 +890,8 @@ void enqueue_join_forward(const JoinShape &s, const slorr_join_tensors_t &t, con
   a.y = y;
   a.z = z;
   // as many blocks as the CUs hold at once, each a run of rows: 16 waves per CU, 24
-  // where the registers allow it (16384 x 1280 bf16: 51.7 us with 16, 45.2 with 24;
-  // the others are no faster or slower, 4096 x 6144 bf16 48.5 and 54.6)
+  // where the registers allow it (16384 x 1280 bf16: 36.6 us with 16, 31.6 with 24;
+  // 4096 x 6144 bf16, whose blocks are 8 waves: 53 us with 8, 41 with 16)
   const int threads = join_threads(s.dim);
   const int waves = s.dim <= 4096 && s.dtype == SLORR_BF16 && !a.b1 && !a.b2 ? 24 : 16;
   a.per_block = std::max<int64_t>(1, cdiv(s.rows, kCus * (waves * 64 / threads)));
