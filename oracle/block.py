@@ -41,10 +41,11 @@ def threshold(p):
     return int(round(p * 65536))
 
 
-def keep_mask(n, p, key, offset, site=0):
-    """Truth values of n elements: the 16-bit number e mod 8 of block e div 8 is at least threshold(p)."""
+def keep_mask(n, p, key, offset, site=0, first=0):
+    """Truth values of the n elements from `first` (a multiple of 8) on: the 16-bit number e mod 8 of block e div 8 is
+    at least threshold(p)."""
     key, off = key % 2 ** 64, (offset + site) % 2 ** 64
-    i = np.arange((n + 7) // 8, dtype=np.uint64)
+    i = np.arange(first // 8, first // 8 + (n + 7) // 8, dtype=np.uint64)
     lo = np.uint64(0xFFFFFFFF)
     words = philox([i & lo, i >> np.uint64(32), np.full_like(i, off & 0xFFFFFFFF), np.full_like(i, off >> 32)],
                    [key & 0xFFFFFFFF, key >> 32])

@@ -11,10 +11,13 @@ autograd plumbing only; every step runs in libslorr.so.
 
 Tensors are float32 or bfloat16, all of a call of one dtype, on one GPU; the
 last dimension is the row. Activations may be strided (a layout that the
-kernels do not read in place is copied); weights are contiguous. Calls run on
+kernels do not read in place is copied); weights are contiguous (one that does
+not start at a multiple of 16 bytes is copied in every call). Calls run on
 the current stream of the tensors' device and can be captured into a graph.
 Gradients are formed for the inputs that require them. Each is written anew by
-fixed-order sums: no atomics, so results repeat bit for bit.
+fixed-order sums: no atomics, so results repeat bit for bit. To capture a
+backward() into a graph, let no eager graph of the same leaves live: torch would
+tie the capture to the stream of the older graph.
 
 Dropout draws its numbers from rng, an int64 tensor (key, offset) on the device,
 and an integer site that sets the calls of one step apart. The backward pass
@@ -107,9 +110,15 @@ def _ffn_block(x, ldx, w_gate, act, lddy=0):
     return _lib.Ffn(x.numel() // dim, dim, inner, _DTYPE[x.dtype], act, ldx, lddy)
 
 
+def _at16(t):
+    """t, or a copy where its values do not start at a multiple of 16 bytes."""
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 def _ffn_forward(x, shape, ldx, w_gate, w_up, w_down, act, keep):
     """y and, with keep, the state of the backward pass. x is laid out by _rows."""
     with _device(x):
+        w_gate, w_up, w_down = _at16(w_gate), _at16(w_up), _at16(w_down)
         d = _ffn_block(x, ldx, w_gate, act)
         st, ws = ctypes.c_size_t(), ctypes.c_size_t()
         check(lib().slorr_ffn_sizes(d, st, ws, None), "slorr_ffn_sizes")
@@ -137,6 +146,7 @@ class _GatedFfn(torch.autograd.Function):
         x, w_gate, w_up, w_down, state = ctx.saved_tensors
         need = ctx.needs_input_grad
         with _device(x):
+            w_gate, w_up, w_down = _at16(w_gate), _at16(w_up), _at16(w_down)
             dy, lddy = _rows(dy, w_gate.shape[1])
             d = _ffn_block(x, ctx.ldx, w_gate, ctx.act, lddy)
             ws = ctypes.c_size_t()
@@ -228,8 +238,7 @@ class _Join(torch.autograd.Function):
 
 
 def _aligned(t: torch.Tensor) -> torch.Tensor:
-    t = t.contiguous()
-    return t if t.data_ptr() % 16 == 0 else t.clone()
+    return _at16(t.contiguous())
 
 
 def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
@@ -240,6 +249,9 @@ def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
         out[1], d.ldf = _rows(out[1], d.dim)
     if out[4] is not None:
         out[4], d.ld_gate = _rows(out[4], d.dim)
+    for i in _VECTORS:
+        if out[i] is not None:
+            out[i] = _at16(out[i])
     return out
 
 
