@@ -20,7 +20,7 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 enum FfnEpi { kStore = 0, kAct = 1, kActBack = 2 };
 
 // The block tiles: 256 x 256 (8 waves of 128 x 64) and 128 x 128 (4 of 64 x 64, two
-// blocks per CU). Microseconds of a round of blocks: per slab of k with every CU
+// blocks per CU; 8 of 32 x 64 where there is one). Microseconds of a round of blocks: per slab of k with every CU
 // at work (alone: with one block per CU at most, where a slab's latency is all
 // there is), and for its start and end (kActBack, which loads and stores five
 // values per sum: back). From 16384 x 1536 x 6144 in bf16, us of a round of each:

@@ -97,7 +97,12 @@ void launch_products(FfnArgs &a, hipStream_t st) {
   a.slabs = int32_t(slabs_of(q[0], F32));
   a.parts = int32_t(c.parts);
   a.per = int32_t(c.per);
+  // 128-tiles of which no CU has two: eight waves of 32 x 64 instead of four of 64 x 64,
+  // so that each SIMD has a second wave while one waits, and a third LDS stage (us of
+  // four waves and eight: 100 x 1536 x 6144 bf16 forward 39.5, 35.4; 501 x 1280 x 3456
+  // forward 37.8, 35.7; 2048 x 576 x 1536 backward 73.5, 69)
   if (c.kind == 0) launch_tiles<0, 2, 4, 2, AK, BK, EPI, F32>(a, st);
+  else if (c.whole + c.tail * c.parts <= kCus) launch_tiles<1, 4, 2, 3, AK, BK, EPI, F32>(a, st);
   else launch_tiles<1, 2, 2, 2, AK, BK, EPI, F32>(a, st);
 }
 
