@@ -421,7 +421,8 @@ typedef enum { SLORR_RMS = 0, SLORR_LAYER = 1 } slorr_norm_t;
  *
  * x is the residual stream, f the block's output. Without f (NULL) y is x and
  * the call is the norm alone. drop is slorr_dropout with the element index
- * row * dim + column. 1 <= dim <= 8192, rows >= 0. */
+ * row * dim + column, as a factor: an infinity or a NaN of f stays a NaN where it
+ * is dropped. 1 <= dim <= 8192, rows >= 0, rows times the longest stride at most 2^50. */
 typedef struct {
   int64_t rows;
   int32_t dim;

@@ -100,7 +100,12 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _bytes(n: int, like: torch.Tensor) -> torch.Tensor:
-    return torch.empty(n, dtype=torch.uint8, device=like.device)
+    return like.new_empty(n, dtype=torch.uint8)
+
+
+def _new(shape, like: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of that shape (empty_like where it can be: the shortest way to one)."""
+    return torch.empty_like(like) if like.shape == shape and like.is_contiguous() else like.new_empty(shape)
 
 
 # ------------------------------------------------------------- feed-forward
@@ -122,7 +127,7 @@ def _ffn_forward(x, shape, ldx, w_gate, w_up, w_down, act, keep):
         d = _ffn_block(x, ldx, w_gate, act)
         st, ws = ctypes.c_size_t(), ctypes.c_size_t()
         check(lib().slorr_ffn_sizes(d, st, ws, None), "slorr_ffn_sizes")
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        y = _new(shape, x)
         state = _bytes(st.value, x) if keep else None
         work = _bytes(ws.value, x)
         check(lib().slorr_ffn_forward(d, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
@@ -151,8 +156,8 @@ class _GatedFfn(torch.autograd.Function):
             d = _ffn_block(x, ctx.ldx, w_gate, ctx.act, lddy)
             ws = ctypes.c_size_t()
             check(lib().slorr_ffn_sizes(d, None, None, ws), "slorr_ffn_sizes")
-            grads = [torch.empty(s, dtype=x.dtype, device=x.device) if n else None
-                     for s, n in zip((ctx.shape, w_gate.shape, w_up.shape, w_down.shape), need)]
+            grads = [_new(ctx.shape, x) if need[0] else None]
+            grads += [torch.empty_like(w) if n else None for w, n in zip((w_gate, w_up, w_down), need[1:])]
             work = _bytes(ws.value, x)
             check(lib().slorr_ffn_backward(d, dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
                                            w_down.data_ptr(), state.data_ptr(), *map(_ptr, grads), work.data_ptr(),
@@ -194,8 +199,8 @@ def _join_run(d, shape, tensors, rng):
     """The forward call on laid-out inputs: y (None without f) and z (None without PRE)."""
     x = tensors[0]
     with _device(x):
-        y = None if tensors[1] is None else torch.empty(shape, dtype=x.dtype, device=x.device)
-        z = torch.empty(shape, dtype=x.dtype, device=x.device) if d.flags & _lib.JOIN_PRE else None
+        y = None if tensors[1] is None else _new(shape, x)
+        z = _new(shape, x) if d.flags & _lib.JOIN_PRE else None
         check(lib().slorr_join_forward(d, _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
                                        _stream(x)), "slorr_join_forward")
     return y, z
@@ -225,9 +230,11 @@ class _Join(torch.autograd.Function):
         with _device(x):
             dy = douts[0] if laid[1] is not None else None
             dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
-            dy, dz = (None if t is None else _aligned(t) for t in (dy, dz))
-            grads = [torch.empty(s, dtype=x.dtype, device=x.device) if n else None
-                     for s, n in zip(ctx.shapes, ctx.needs_input_grad[2:])]
+            if dy is not None:
+                dy = _aligned(dy)
+            if dz is not None:
+                dz = _aligned(dz)
+            grads = [_new(s, t) if n else None for s, t, n in zip(ctx.shapes, laid, ctx.needs_input_grad[2:])]
             ws = ctypes.c_size_t()
             check(lib().slorr_join_workspace(d, ws), "slorr_join_workspace")
             work = _bytes(ws.value, x)
@@ -238,7 +245,7 @@ class _Join(torch.autograd.Function):
 
 
 def _aligned(t: torch.Tensor) -> torch.Tensor:
-    return _at16(t.contiguous())
+    return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else _at16(t.contiguous())
 
 
 def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
@@ -334,7 +341,8 @@ def block_join(x: torch.Tensor, f: torch.Tensor, *, post: Optional[bool] = None,
     default where one of its vectors is given. Vectors and scale: (dim,). gate:
     (dim,), x's shape, or x's shape with trailing dimensions before the last set
     to 1 (one gate row per sequence). p, rng, site: residual dropout, as in
-    dropout()."""
+    dropout(), as a factor 0 or 1 / (1 - p): an infinite u stays a NaN where it is
+    dropped."""
     _check_first(x, "x")
     if f is None:
         raise ValueError("f is required (block_norm is the norm alone)")
