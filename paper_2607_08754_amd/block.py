@@ -15,7 +15,8 @@ kernels do not read in place is copied); weights are contiguous (one that does
 not start at a multiple of 16 bytes is copied in every call). Calls run on
 the current stream of the tensors' device and can be captured into a graph.
 Gradients are formed for the inputs that require them. Each is written anew by
-fixed-order sums: no atomics, so results repeat bit for bit. To capture a
+fixed-order sums: no atomics, so results repeat bit for bit. They can be taken
+once: differentiating them again raises RuntimeError. To capture a
 backward() into a graph, let no eager graph of the same leaves live: torch would
 tie the capture to the stream of the older graph.
 
@@ -32,7 +33,6 @@ import math
 from typing import List, Optional, Tuple
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import _lib
 from ._lib import check, lib
@@ -78,6 +78,31 @@ def _rows(t: torch.Tensor, dim: int) -> Tuple[torch.Tensor, int]:
         m = m.clone(memory_format=torch.contiguous_format)
         ld = dim
     return m, ld if n > 1 else dim
+
+
+class _Once(torch.autograd.Function):
+    """Gradients as they are, which refuse to be differentiated (anchor requires a gradient)."""
+
+    @staticmethod
+    def forward(ctx, anchor, *grads):
+        return grads
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the block operators' gradients can be taken once only")
+
+
+def _once(backward):
+    """A backward pass whose results, where a graph of them is asked for (create_graph), end in _Once."""
+
+    def run(ctx, *grads):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        return _Once.apply(torch.empty(0, requires_grad=True), *out)
+
+    return run
 
 
 _HERE = contextlib.nullcontext()
@@ -146,7 +171,7 @@ class _GatedFfn(torch.autograd.Function):
         return y
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dy):
         x, w_gate, w_up, w_down, state = ctx.saved_tensors
         need = ctx.needs_input_grad
@@ -221,7 +246,7 @@ class _Join(torch.autograd.Function):
         return (y, z) if y is not None and z is not None else z if y is None else y
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, *douts):
         rng, *laid = ctx.saved_tensors
         d, x = ctx.d, laid[0]
@@ -377,7 +402,7 @@ class _Dropout(torch.autograd.Function):
         return _dropout_run(x, p, rng, site)
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dy):
         return _dropout_run(dy, ctx.p, ctx.saved_tensors[0], ctx.site), None, None, None
 

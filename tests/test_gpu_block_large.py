@@ -192,3 +192,18 @@ def test_captured_backward_into_grad():
         with torch.no_grad():
             gated = block(x)
         assert bool(torch.isfinite(gated).all())
+
+
+def test_gradients_are_differentiable_once():
+    """create_graph gives the gradients; differentiating them again is refused."""
+    import torch
+    from paper_2607_08754_amd import block_join, dropout, gated_ffn
+    x, w, dy = _ffn_inputs(20, 24, 32, "f32", 4)
+    x = x.requires_grad_()
+    rng = torch.tensor([1, 2], dtype=torch.int64, device=DEV)
+    for f in (lambda: gated_ffn(x, *w), lambda: block_join(x, x * 2, pre=True)[1], lambda: dropout(x, 0.5, rng)):
+        want = torch.autograd.grad(f(), x, dy)[0]
+        got = torch.autograd.grad(f(), x, dy, create_graph=True)[0]
+        assert torch.equal(got, want)
+        with pytest.raises(RuntimeError, match="once only"):
+            got.sum().backward()
