@@ -20,7 +20,13 @@ constexpr int64_t kMaxWidth = int64_t(1) << 20;      // dim, inner
 constexpr int64_t kMaxStride = (int64_t(1) << 22) - 8;   // row strides, in elements: the 256 rows
                                                      // of a tile stay within 2 GiB
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1024;
-constexpr int kFewTokens = 64;                       // forward alone: k_few up to here
+// Forward alone: k_few up to 64 tokens, in bf16 beyond 16 while tokens * dim * inner
+// stays below kFewWork: it reads the tokens in every block, k_ffn's tiles do not (us
+// of k_few and k_ffn in bf16: 32 tokens of 1536 x 6144 33.7, 34.6, 64 of them 50, 35;
+// 64 of 1280 x 3456 29.0, 29.2; 16 of 4096 x 11008 62, 71, 24 of them 75, 71; in
+// fp32 64 of 4096 x 11008 285, 596).
+constexpr int kFewTokens = 64;
+constexpr int64_t kFewWork = 300000000;
 constexpr int kMaxNorm = 8192;                       // dim of a join: 512 threads, two pieces of 8 each
 
 inline int64_t up8(int64_t n) { return (n + 7) & ~int64_t(7); }
@@ -32,7 +38,9 @@ struct FfnShape {
   size_t elem() const { return dtype == SLORR_F32 ? 4 : 2; }
   int64_t ldf() const { return up8(inner); }         // rows of the inner tensors
   int64_t ldd() const { return up8(dim); }
-  bool few() const { return tokens <= kFewTokens; }
+  bool few() const {
+    return tokens <= kFewTokens && (dtype == SLORR_F32 || tokens <= 16 || tokens * dim * inner <= kFewWork);
+  }
   // operands that are read in place: bf16 rows of whole chunks
   bool direct(int64_t width, int64_t ld) const { return dtype == SLORR_BF16 && width % 8 == 0 && ld % 8 == 0; }
 };

@@ -642,9 +642,11 @@ __global__ __launch_bounds__(256) void k_tail(FfnArgs args) {
 // (lane l: row l % 16, k from 8 (l / 16) on; fp32: four k of 4 (l / 16) on in
 // four instructions), the tokens are the other operand, read through the caches
 // by every block. The waves' sums meet in LDS. No row alignment is needed. One token
-// of 1536 x 6144 in bf16: 38 MB of Wg and Wu in 11.1 us, 19 MB of Wd in 9.0 (the
+// of 1536 x 6144 in bf16: 38 MB of Wg and Wu in 10.8 us, 19 MB of Wd in 8.9 (the
 // copy's rate would take 7.7 and 3.9; the rest is the start of a launch, one trip to
-// HBM and the sums' way through LDS). The tiles of k_ffn took 97 us for both.
+// HBM and the sums' way through LDS). The tiles of k_ffn take 33 us for both. Not
+// kept: chunks loaded one to three ahead (19.0 against 18.6 us), blocks that begin at
+// different chunks (no change).
 struct FewArgs {
   const void *x, *w0, *w1;
   void *out;                   // h or y
@@ -686,15 +688,20 @@ __global__ __launch_bounds__(TF > 2 ? 512 : 1024) void k_few(FewArgs a) {
       return get(row, k, a.k).q[0];
     }
   };
-  for (int k0 = wave * kChunk; k0 < a.k; k0 += waves * kChunk) {
-    u32x4 fw[2][NF], fx[2][TF];
+  struct Chunk {
+    u32x4 w[2][NF], x[2][TF];
+  } c;
+  auto whole = [](const T *row, int k) { return u32x4(*(const SLORR_GLOBAL u32x4_any *)(row + k)); };
+  auto fetch = [&](int k, auto get) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
 #pragma unroll
-      for (int i = 0; i < NF; ++i) fw[s][i] = load(w[i], k0 + s * kStep + kl);
+      for (int i = 0; i < NF; ++i) c.w[s][i] = get(w[i], k + s * kStep + kl);
 #pragma unroll
-      for (int t = 0; t < TF; ++t) fx[s][t] = load(x[t], k0 + s * kStep + kl);
+      for (int t = 0; t < TF; ++t) c.x[s][t] = get(x[t], k + s * kStep + kl);
     }
+  };
+  auto multiply = [&]() {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -704,13 +711,24 @@ __global__ __launch_bounds__(TF > 2 ? 512 : 1024) void k_few(FewArgs a) {
           if constexpr (F32) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fw[s][i][j]), __uint_as_float(fx[s][t][j]),
+              acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(c.w[s][i][j]), __uint_as_float(c.x[s][t][j]),
                                                                acc[i][t], 0, 0, 0);
           } else {
-            acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[s][i]),
-                                                                __builtin_bit_cast(bf16x8, fx[s][t]), acc[i][t], 0, 0, 0);
+            acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, c.w[s][i]),
+                                                                __builtin_bit_cast(bf16x8, c.x[s][t]), acc[i][t], 0, 0, 0);
           }
         }
+  };
+  // whole chunks without the code for a row's end, then that end by the wave whose
+  // turn it is
+  for (int k = wave * kChunk; k + kChunk <= a.k; k += waves * kChunk) {
+    fetch(k, whole);
+    multiply();
+  }
+  const int end = a.k / kChunk;
+  if (end * kChunk < a.k && end % waves == wave) {
+    fetch(end * kChunk, load);
+    multiply();
   }
 #pragma unroll
   for (int i = 0; i < NF; ++i)

@@ -207,3 +207,13 @@ def test_gradients_are_differentiable_once():
         assert torch.equal(got, want)
         with pytest.raises(RuntimeError, match="once only"):
             got.sum().backward()
+
+
+@pytest.mark.parametrize("T,dtype", [(1, "bf16"), (16, "bf16"), (17, "bf16"), (40, "bf16"), (64, "f32")])
+def test_ffn_few_tokens_of_wide_layers(T, dtype):
+    """Either side of the size from which a few tokens take the tiles."""
+    from paper_2607_08754_amd import gated_ffn
+    d, n = 1800, 6001
+    x, w, dy = _ffn_inputs(T, d, n, dtype, T)
+    g, tol = bounds(*map(_np, (x, *w, dy)), "silu", dtype)
+    check("y", gated_ffn(x, *w), g.fwd.y, tol["y"], dtype, max(d, n))
