@@ -596,6 +596,14 @@ void k_join_bwd(JoinArgs a) {
         if constexpr (kLdsP) add(3, v, ey, sw2.v[v]);
         if constexpr (BIAS) add(1, v, e.v[v], sb2.v[v]);
       }
+      if (a.layer) {
+        // the mean went out of columns past dim as well, and the post norm sums d over a
+        // row: zeros there again (masked here, not above: no register more is held)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d.v[v][j] = column(v) + (WHOLE ? 0 : j) < a.dim ? d.v[v][j] : 0.0f;
+      }
     }
     if (!kAhead && !a.dz) take_dy();
     if (a.dx) {
