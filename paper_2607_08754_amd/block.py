@@ -121,7 +121,28 @@ def _stream(t: torch.Tensor) -> int:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return None
+    p = t.data_ptr()
+    if not p and t.numel():                       # (to the library a null pointer is an absent tensor)
+        raise ValueError("a tensor has no memory")
+    return p
+
+
+def _save(ctx, *tensors) -> None:
+    ctx.save_for_backward(*tensors)
+    ctx.kinds = [None if t is None else (t.shape, t.dtype, t.device) for t in tensors]
+
+
+def _saved(ctx):
+    """The saved tensors. saved_tensors_hooks may return them at other addresses and
+    in other layouts, so the backward calls lay them out again; anything else about
+    them has to be as it was."""
+    tensors = ctx.saved_tensors
+    for t, kind in zip(tensors, ctx.kinds):
+        if kind is not None and (t.shape, t.dtype, t.device) != kind:
+            raise RuntimeError(f"a saved tensor of {kind[1]} {tuple(kind[0])} on {kind[2]} came back as {t.dtype} {tuple(t.shape)} on {t.device}")
+    return tensors
 
 
 def _bytes(n: int, like: torch.Tensor) -> torch.Tensor:
@@ -166,19 +187,20 @@ class _GatedFfn(torch.autograd.Function):
     def forward(ctx, x, w_gate, w_up, w_down, act):
         rows, ldx = _rows(x, w_gate.shape[1])
         y, state = _ffn_forward(rows, x.shape, ldx, w_gate, w_up, w_down, act, True)
-        ctx.act, ctx.ldx, ctx.shape = act, ldx, x.shape
-        ctx.save_for_backward(rows, w_gate, w_up, w_down, state)
+        ctx.act, ctx.shape = act, x.shape
+        _save(ctx, rows, w_gate, w_up, w_down, state)
         return y
 
     @staticmethod
     @_once
     def backward(ctx, dy):
-        x, w_gate, w_up, w_down, state = ctx.saved_tensors
+        x, w_gate, w_up, w_down, state = _saved(ctx)
         need = ctx.needs_input_grad
         with _device(x):
-            w_gate, w_up, w_down = _at16(w_gate), _at16(w_up), _at16(w_down)
+            x, ldx = _rows(x, w_gate.shape[1])
+            w_gate, w_up, w_down, state = _aligned(w_gate), _aligned(w_up), _aligned(w_down), _aligned(state)
             dy, lddy = _rows(dy, w_gate.shape[1])
-            d = _ffn_block(x, ctx.ldx, w_gate, ctx.act, lddy)
+            d = _ffn_block(x, ldx, w_gate, ctx.act, lddy)
             ws = ctypes.c_size_t()
             check(lib().slorr_ffn_sizes(d, None, None, ws), "slorr_ffn_sizes")
             grads = [_new(ctx.shape, x) if need[0] else None]
@@ -241,18 +263,20 @@ class _Join(torch.autograd.Function):
         y, z = _join_run(d, tensors[0].shape, laid, rng)
         ctx.d = d
         ctx.shapes = [None if t is None else t.shape for t in tensors]
-        ctx.save_for_backward(rng, *laid)
+        _save(ctx, rng, *laid)
         ctx.set_materialize_grads(False)
         return (y, z) if y is not None and z is not None else z if y is None else y
 
     @staticmethod
     @_once
     def backward(ctx, *douts):
-        rng, *laid = ctx.saved_tensors
-        d, x = ctx.d, laid[0]
+        rng, *laid = _saved(ctx)
         if all(t is None for t in douts):
             return (None,) * (2 + len(laid))
-        with _device(x):
+        d = _lib.Join.from_buffer_copy(ctx.d)
+        with _device(laid[0]):
+            laid = _join_layout(d, laid)
+            x, rng = laid[0], None if rng is None else _aligned(rng)
             dy = douts[0] if laid[1] is not None else None
             dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
             if dy is not None:
@@ -283,7 +307,7 @@ def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
         out[4], d.ld_gate = _rows(out[4], d.dim)
     for i in _VECTORS:
         if out[i] is not None:
-            out[i] = _at16(out[i])
+            out[i] = _aligned(out[i])
     return out
 
 
@@ -398,13 +422,14 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, p, rng, site):
         ctx.p, ctx.site = p, site
-        ctx.save_for_backward(rng)
+        _save(ctx, rng)
         return _dropout_run(x, p, rng, site)
 
     @staticmethod
     @_once
     def backward(ctx, dy):
-        return _dropout_run(dy, ctx.p, ctx.saved_tensors[0], ctx.site), None, None, None
+        rng, = _saved(ctx)
+        return _dropout_run(dy, ctx.p, None if rng is None else _aligned(rng), ctx.site), None, None, None
 
 
 def dropout(x: torch.Tensor, p: float, rng: Optional[torch.Tensor], site: int = 0) -> torch.Tensor:
