@@ -16,7 +16,8 @@ not start at a multiple of 16 bytes is copied in every call). Calls run on
 the current stream of the tensors' device and can be captured into a graph.
 Gradients are formed for the inputs that require them. Each is written anew by
 fixed-order sums: no atomics, so results repeat bit for bit. They can be taken
-once: differentiating them again raises RuntimeError. To capture a
+once: differentiating them again raises RuntimeError, and so do forward-mode
+derivatives and tracing (torch.jit.trace, make_fx). To capture a
 backward() into a graph, let no eager graph of the same leaves live: torch would
 tie the capture to the stream of the older graph.
 
@@ -33,6 +34,7 @@ import math
 from typing import List, Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import check, lib
@@ -45,6 +47,21 @@ _NORM = {"rms": _lib.RMS, "layer": _lib.LAYER}
 _MAX_STRIDE = (1 << 22) - 8
 _MAX_NORM = 8192
 _MOST_P = (65535.5 - 2.0 ** -20) / 65536          # p counts in steps of 2^-16
+
+
+_is_tracing = getattr(torch._C, "_is_tracing", torch.jit.is_tracing)           # (without its Python frame)
+_modes = getattr(torch._C, "_len_torch_dispatch_stack", lambda: 0)
+
+
+def _check_transforms(*tensors) -> None:
+    """Refuses what cannot see the kernels: forward-mode derivatives, whose tangents
+    would be lost, and traces, which would hold the outputs' allocation alone."""
+    if _is_tracing() or (_modes() and torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None):
+        raise RuntimeError("the block operators cannot be traced (a captured graph holds them)")
+    if forward_ad._current_level >= 0:
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+                raise RuntimeError("the block operators have no forward-mode derivative")
 
 
 def _check_first(x: torch.Tensor, name: str) -> None:
@@ -96,6 +113,7 @@ def _once(backward):
     """A backward pass whose results, where a graph of them is asked for (create_graph), end in _Once."""
 
     def run(ctx, *grads):
+        _check_transforms(*grads)
         if not torch.is_grad_enabled():
             return backward(ctx, *grads)
         with torch.no_grad():
@@ -219,6 +237,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     w_gate, w_up: (inner, dim), w_down: (dim, inner), contiguous. act: "silu",
     "gelu" or "gelu_tanh". In bfloat16 the inner activations are rounded to
     bfloat16 between the products. Without gradients nothing is kept."""
+    _check_transforms(x, w_gate, w_up, w_down)
     _check_first(x, "x")
     if act not in _ACT:
         raise ValueError(f"act must be one of {list(_ACT)}")
@@ -372,6 +391,7 @@ def block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                kind: str = "rms", eps: float = 1e-5) -> torch.Tensor:
     """The norm of a block's input over the last dimension (at most 8192):
     kind "rms" or "layer", times weight plus bias (each (dim,) or None)."""
+    _check_transforms(x, weight, bias)
     _check_first(x, "x")
     return _join_call(x, None, kind, eps, False, True, (x, None, None, None, None, None, weight, bias), 1.0, 0.0, None, 0)
 
@@ -392,6 +412,7 @@ def block_join(x: torch.Tensor, f: torch.Tensor, *, post: Optional[bool] = None,
     to 1 (one gate row per sequence). p, rng, site: residual dropout, as in
     dropout(), as a factor 0 or 1 / (1 - p): an infinite u stays a NaN where it is
     dropped."""
+    _check_transforms(x, f, post_weight, post_bias, gate, scale, pre_weight, pre_bias)
     _check_first(x, "x")
     if f is None:
         raise ValueError("f is required (block_norm is the norm alone)")
@@ -437,6 +458,7 @@ def dropout(x: torch.Tensor, p: float, rng: Optional[torch.Tensor], site: int = 
     order) is kept by its 16-bit number of the Philox4x32-10 sequence with key
     rng[0] and offset rng[1] + site, so p counts in steps of 2^-16 (rounded to
     the nearest; the factor is that of the rounded p)."""
+    _check_transforms(x)
     _check_first(x, "x")
     _check_rng(p, rng, x)
     if torch.is_grad_enabled() and x.requires_grad:

@@ -149,6 +149,15 @@ def test_other_saved_tensors_are_refused(lib, op, what):
     assert [c for c in lib.calls[n:] if c != "dropout"] == [] and lib.calls[n:].count("dropout") <= 1
 
 
+@pytest.mark.parametrize("create", [False, True])
+def test_a_tangent_of_the_output_gradient_is_refused(lib, create):
+    import torch.autograd.forward_ad as fw
+    x = torch.randn(6, 16).requires_grad_()
+    y = block._Dropout.apply(x, 0.5, torch.zeros(2, dtype=torch.int64), 0)
+    with fw.dual_level(), pytest.raises(RuntimeError, match="forward-mode"):
+        torch.autograd.grad(y, x, fw.make_dual(torch.ones_like(y), torch.ones_like(y)), create_graph=create)
+
+
 def test_tensors_without_memory_are_refused(lib):
     """A vector whose storage was released is not an absent one."""
     x = torch.randn(6, 16)
