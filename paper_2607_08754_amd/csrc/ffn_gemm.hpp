@@ -57,7 +57,8 @@ __device__ __forceinline__ void act_and_slope(float a, float &f, float &s) {
     f = a * c;
     s = c + a * (F32 ? expf(-0.5f * a * a) : __expf(-0.5f * a * a)) * 0.39894228040143268f;
   } else {                     // 0.5 a (1 + tanh u) = a sigmoid(2 u)
-    const float k = 1.5957691216057308f, q = 0.044715f * a * a;
+    // (a^2 held below infinity: g is 0 or 1 long before, and the slope has 0 times it)
+    const float k = 1.5957691216057308f, q = fminf(0.044715f * a * a, 1e30f);
     const float g = sigmoid<F32>(k * a * (1.0f + q));
     f = a * g;
     s = g + f * (1.0f - g) * k * (1.0f + 3.0f * q);
