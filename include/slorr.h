@@ -388,8 +388,10 @@ SLORR_API slorr_status_t slorr_ffn_sizes(const slorr_ffn_t *block, size_t *state
 /* Forward. state: 16-byte aligned, or NULL where no backward follows.
  * workspace: 256-byte aligned, workspace_bytes at least slorr_ffn_sizes'. In
  * BF16, h is rounded to bf16 before its product with Wd. F32 products are sums
- * of six bf16 products that together carry fp32's 24 bits; an infinity in an
- * F32 operand gives NaN. tokens == 0 writes nothing.
+ * of six bf16 products that together carry fp32's 24 bits of values from 2^-110 on
+ * (smaller ones are off by up to 2^-134), and an infinity in an operand gives NaN
+ * (a call of up to 64 tokens without state forms fp32 products: there it stays one).
+ * tokens == 0 writes nothing.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED (dtype, act, limits), WORKSPACE, HIP. */
 SLORR_API slorr_status_t slorr_ffn_forward(const slorr_ffn_t *block, const void *x, const void *w_gate,
                                  const void *w_up, const void *w_down, void *y, void *state,
@@ -407,7 +409,9 @@ SLORR_API slorr_status_t slorr_ffn_backward(const slorr_ffn_t *block, const void
                                  void *dw_down, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Norm over a row t of dim values: RMS t / sqrt(mean(t^2) + eps); LAYER
- * (t - mean(t)) / sqrt(var(t) + eps) with the biased variance. */
+ * (t - mean(t)) / sqrt(var(t) + eps) with the biased variance. The squares are
+ * summed in fp32: a row's sum has to stay below 2^128 (beyond it the norm is 0), and
+ * its mean plus eps at or above 2^-126. */
 typedef enum { SLORR_RMS = 0, SLORR_LAYER = 1 } slorr_norm_t;
 
 #define SLORR_JOIN_POST 0x1u     /* norm of f (post_weight, post_bias)                    */

@@ -236,7 +236,9 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
 
     w_gate, w_up: (inner, dim), w_down: (dim, inner), contiguous. act: "silu",
     "gelu" or "gelu_tanh". In bfloat16 the inner activations are rounded to
-    bfloat16 between the products. Without gradients nothing is kept."""
+    bfloat16 between the products. In float32 an infinity comes out as a NaN,
+    but for calls of up to 64 tokens without gradients, where it stays one.
+    Without gradients nothing is kept."""
     _check_transforms(x, w_gate, w_up, w_down)
     _check_first(x, "x")
     if act not in _ACT:
