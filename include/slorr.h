@@ -462,7 +462,8 @@ typedef struct {
 SLORR_API slorr_status_t slorr_join_forward(const slorr_join_t *join, const slorr_join_tensors_t *in,
                                  const int64_t *rng, void *y, void *z, void *stream);
 
-/* Device workspace of slorr_join_backward, never 0. Host only. */
+/* Device workspace of slorr_join_backward, never 0 and below 128 MiB whatever the
+ * sizes. Host only. */
 SLORR_API slorr_status_t slorr_join_workspace(const slorr_join_t *join, size_t *bytes);
 
 /* Backward: the gradients of sum(dy * y) + sum(dz * z), dy and dz contiguous, either

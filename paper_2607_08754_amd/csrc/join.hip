@@ -385,8 +385,9 @@ __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
 }
 
 // Gate rows against a block's rows: one gate row (or none) for all of them, a
-// gate row for each, or several gate rows of several rows each.
-enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2 };
+// gate row for each, or several gate rows of several rows each (kGroups; kRuns with
+// two pieces per thread).
+enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2, kRuns = 3 };
 
 // A block takes consecutive rows: whole groups (the rows of one gate row), or a
 // part of one group where there are fewer groups than blocks. Column sums stay
@@ -396,7 +397,9 @@ enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2 };
 // M f^ and Q = sum dY M, the sums of scale, post_weight and post_bias are k times
 // g (w1 P + b1 Q), s g P and s g Q (kOneGate's g; else 1), and one gate row's is
 // k s (w1 P + b1 Q). So a row adds to P, and Q where there are biases (BIAS), and
-// to dz y^ and dz; several gate rows add a sum of their own.
+// to dz y^ and dz; several gate rows add a sum of their own (kGroups). Two pieces per
+// thread leave no registers for that one: kRuns takes P and Q as of one gate row, and at
+// the end of its rows adds what they give to the block's partial rows in memory.
 //
 // A row has three block sums one after the other (RMS; LAYER five): the next
 // row is loaded before them, and the y norm's two sums share one.
@@ -414,6 +417,7 @@ void k_join_bwd(JoinArgs a) {
   // two pieces per thread: the biases' sums (beside a gate per row all sums) in LDS,
   // each thread its own slots; the registers hold no more
   constexpr bool kLds = NV > 1 && BIAS, kLdsP = kLds && MODE != kOneGate;
+  constexpr bool kOne = MODE == kOneGate || MODE == kRuns;       // a gate row for many rows
   constexpr int kSlots = kLdsP ? 4 : kLds ? 2 : 0;
   Row<NV> P = {}, Q = {}, sw2 = {}, sb2 = {}, sg = {};
   __shared__ float4v sums[kLds ? kSlots * 2 * NV * 512 : 1];
@@ -450,9 +454,43 @@ void k_join_bwd(JoinArgs a) {
   const int64_t g1 = a.parts > 1 ? g0 + 1 : min(a.groups, g0 + a.gpb);
   const int64_t r0 = g0 * a.rpg + (a.parts > 1 ? (blk - g0 * a.parts) * a.rpp : 0);
   const int64_t r1 = a.parts > 1 ? min(r0 + a.rpp, g1 * a.rpg) : g1 * a.rpg;
-  int64_t gate_row = MODE == kEachRow ? r0 : MODE == kGroups ? g0 : a.gate && r0 < r1 ? r0 / a.gate_run : 0;
-  int64_t group_end = MODE == kGroups ? (g0 + 1) * a.rpg : 0;
-  const T *gate0 = MODE == kOneGate && a.gate ? static_cast<const T *>(a.gate) + gate_row * a.ldg : nullptr;
+  int64_t gate_row = MODE == kEachRow ? r0 : MODE == kGroups || MODE == kRuns ? g0 : a.gate && r0 < r1 ? r0 / a.gate_run : 0;
+  int64_t group_end = MODE == kGroups || MODE == kRuns ? (g0 + 1) * a.rpg : 0;
+  const T *gate0 = kOne && a.gate ? static_cast<const T *>(a.gate) + gate_row * a.ldg : nullptr;
+  // what P and Q give: a part of the gate row's sum (kRuns: the sum), and parts of those of
+  // scale, post_weight and post_bias. fresh: the first ones of the block
+  const int64_t step = int64_t(gridDim.x) * a.ldp;
+  auto leave = [&](int v, bool fresh) {
+    float w[8], b[8], s[8], g[8], t[3][8], dg[8];
+    take(0, v, Q.v[v]);
+    if constexpr (kLdsP) take(2, v, P.v[v]);
+    vector8<T, WHOLE>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
+    vector8<T, WHOLE>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
+    vector8<T, WHOLE>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
+    vector8<T, WHOLE>(unmoved(gate0), column(v), a.dim, 1.0f, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float q = a.k * (BIAS ? fmaf(w[j], P.v[v][j], b[j] * Q.v[v][j]) : w[j] * P.v[v][j]);
+      t[0][j] = a.k * s[j] * g[j] * P.v[v][j];
+      t[1][j] = a.k * s[j] * g[j] * Q.v[v][j];
+      t[2][j] = g[j] * q;
+      dg[j] = s[j] * q;
+    }
+    if (kOne && a.gpart) put(a.gpart + blk * a.ldp, column(v), a.ldp, dg);
+    if (MODE == kRuns && a.dgate) put_piece<WHOLE>(static_cast<T *>(a.dgate) + gate_row * a.dim, column(v), a.dim, dg);
+    if (!a.part) return;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      float *p = a.part + blk * a.ldp + i * step;
+      if (MODE == kRuns && !fresh) {
+        float o[8];
+        widen<float>(get(p, column(v), a.ldp), o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[i][j] += o[j];
+      }
+      put(p, column(v), a.ldp, t[i]);
+    }
+  };
   Raw<T> nx[NV], nf[NV], nd[NV], nz[NV], ng[NV];
   // two pieces per thread: no loads ahead, each operand not before it is needed,
   // the vectors' products and the dropout factors formed at each use
@@ -465,7 +503,7 @@ void k_join_bwd(JoinArgs a) {
   auto fetch_gate = [&](int64_t gr) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if constexpr (MODE != kOneGate) ng[v] = piece_of<WHOLE>(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
+      if constexpr (!kOne) ng[v] = piece_of<WHOLE>(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
   };
   auto fetch = [&](int64_t row, int64_t gr) {
 #pragma unroll
@@ -473,7 +511,7 @@ void k_join_bwd(JoinArgs a) {
       nx[v] = piece_of<WHOLE>(static_cast<const T *>(a.x) + row * a.ldx, column(v), a.dim);
       if (a.f) nf[v] = piece_of<WHOLE>(static_cast<const T *>(a.f) + row * a.ldf, column(v), a.dim);
       if (a.dz) nz[v] = piece_of<WHOLE>(static_cast<const T *>(a.dz) + row * a.dim, column(v), a.dim);
-      if constexpr (!kAhead && MODE != kOneGate)
+      if constexpr (!kAhead && !kOne)
         ng[v] = piece_of<WHOLE>(static_cast<const T *>(a.gate) + gr * a.ldg, column(v), a.dim);
     }
     if (kAhead) {
@@ -497,6 +535,20 @@ void k_join_bwd(JoinArgs a) {
   for (int64_t row = r0; row < r1; ++row) {
     // the next row's gate row
     const bool turns = MODE == kEachRow || (MODE == kGroups && row + 1 == group_end);
+    if constexpr (MODE == kRuns) {
+      if (row == group_end) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          leave(v, group_end == r0 + a.rpg);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) P.v[v][j] = Q.v[v][j] = 0.0f;
+          if constexpr (kLds) slot(0, v, 0) = slot(0, v, 1) = slot(2, v, 0) = slot(2, v, 1) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        ++gate_row;
+        gate0 += a.ldg;
+        group_end += a.rpg;
+      }
+    }
     const int64_t this_gate = gate_row;
     if (turns) ++gate_row;
     if (MODE == kGroups && turns) group_end += a.rpg;
@@ -508,7 +560,7 @@ void k_join_bwd(JoinArgs a) {
       widen<T>(nx[v], y.v[v]);
       if (a.f) widen<T>(nf[v], u.v[v]);
       if (a.dz) widen<T>(nz[v], e.v[v]);
-      if constexpr (MODE != kOneGate) widen<T>(ng[v], g.v[v]);
+      if constexpr (!kOne) widen<T>(ng[v], g.v[v]);
     }
     auto take_dy = [&]() {
       if (!kAhead) {
@@ -551,7 +603,7 @@ void k_join_bwd(JoinArgs a) {
           if (!kAhead) factors<NV == 1>(a, rng, row, column(v), 1.0f, m.v[v]);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float km = MODE == kOneGate ? a.k * m.v[v][j] : a.k * m.v[v][j] * g.v[v][j];
+            const float km = kOne ? a.k * m.v[v][j] : a.k * m.v[v][j] * g.v[v][j];
             y.v[v][j] = fmaf(km, BIAS ? fmaf(u.v[v][j], sgw.v[v][j], sgb.v[v][j]) : u.v[v][j] * sgw.v[v][j], y.v[v][j]);
           }
         }
@@ -619,7 +671,7 @@ void k_join_bwd(JoinArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         d.v[v][j] *= m.v[v][j];                                  // dY D
-        if constexpr (MODE != kOneGate) {
+        if constexpr (!kOne) {
           const float t = a.k * d.v[v][j];
           dg[j] = t * (BIAS ? fmaf(u.v[v][j], sgw.v[v][j], sgb.v[v][j]) : u.v[v][j] * sgw.v[v][j]);
           if constexpr (MODE == kGroups) dg[j] = sg.v[v][j] += dg[j];
@@ -633,7 +685,7 @@ void k_join_bwd(JoinArgs a) {
       // du w1 = k dY M s g w1
 #pragma unroll
       for (int j = 0; j < 8; ++j) d.v[v][j] *= a.k * sgw.v[v][j];
-      if constexpr (MODE != kOneGate) {
+      if constexpr (!kOne) {
         if (turns) {
           if (a.dgate) put_piece<WHOLE>(static_cast<T *>(a.dgate) + this_gate * a.dim, column(v), a.dim, dg);
           if constexpr (MODE == kGroups) {
@@ -665,38 +717,15 @@ void k_join_bwd(JoinArgs a) {
     }
   }
 
-  if (!a.part && !a.gpart) return;
-  const int64_t step = int64_t(gridDim.x) * a.ldp;
+  if (MODE != kRuns && !a.part && !a.gpart) return;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    float w[8], b[8], s[8], g[8], t1[8], t2[8], t3[8], dg[8];
-    take(0, v, Q.v[v]);
+    leave(v, MODE != kRuns || group_end == r0 + a.rpg);
+    if (!a.part) continue;
     take(1, v, sb2.v[v]);
-    if constexpr (kLdsP) {
-      take(2, v, P.v[v]);
-      take(3, v, sw2.v[v]);
-    }
-    vector8<T, WHOLE>(unmoved(a.w1), column(v), a.dim, 1.0f, w);
-    vector8<T, WHOLE>(unmoved(a.b1), column(v), a.dim, 0.0f, b);
-    vector8<T, WHOLE>(unmoved(a.scale), column(v), a.dim, 1.0f, s);
-    vector8<T, WHOLE>(unmoved(gate0), column(v), a.dim, 1.0f, g);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float q = a.k * (BIAS ? fmaf(w[j], P.v[v][j], b[j] * Q.v[v][j]) : w[j] * P.v[v][j]);
-      t1[j] = a.k * s[j] * g[j] * P.v[v][j];
-      t2[j] = a.k * s[j] * g[j] * Q.v[v][j];
-      t3[j] = g[j] * q;
-      dg[j] = s[j] * q;
-    }
-    if (MODE == kOneGate && a.gpart) put(a.gpart + blk * a.ldp, column(v), a.ldp, dg);
-    if (a.part) {
-      float *p = a.part + blk * a.ldp;
-      put(p, column(v), a.ldp, t1);
-      put(p + step, column(v), a.ldp, t2);
-      put(p + 2 * step, column(v), a.ldp, t3);
-      put(p + 3 * step, column(v), a.ldp, sw2.v[v]);
-      put(p + 4 * step, column(v), a.ldp, sb2.v[v]);
-    }
+    if constexpr (kLdsP) take(3, v, sw2.v[v]);
+    put(a.part + blk * a.ldp + 3 * step, column(v), a.ldp, sw2.v[v]);
+    put(a.part + blk * a.ldp + 4 * step, column(v), a.ldp, sb2.v[v]);
   }
 }
 
@@ -850,7 +879,7 @@ void launch_backward_as(const JoinArgs &a, int64_t blocks, hipStream_t st) {
 template <typename T, int NV>
 void launch_backward_of(const JoinArgs &a, int mode, int64_t blocks, hipStream_t st) {
   if (mode == kEachRow) launch_backward_as<T, NV, kEachRow>(a, blocks, st);
-  else if (NV == 1 && mode == kGroups) launch_backward_as<T, 1, kGroups>(a, blocks, st);
+  else if (mode == kGroups) launch_backward_as<T, NV, NV == 1 ? kGroups : kRuns>(a, blocks, st);
   else launch_backward_as<T, NV, kOneGate>(a, blocks, st);
 }
 template <typename T>
@@ -872,12 +901,7 @@ JoinCut join_cut(const JoinShape &s) {
   const bool summed = s.gate_rows > 1 && s.gate_rows < s.rows;     // gate rows of several tokens each
   c.groups = summed ? s.gate_rows : 1;
   c.rows_per_group = s.rows / c.groups;
-  if (c.groups >= target && s.dim > 4096) {
-    // two pieces per thread leave no registers for a gate's own sums
-    c.parts = c.groups_per_block = 1;
-    c.rows_per_part = c.rows_per_group;
-    c.blocks = c.groups;
-  } else if (c.groups >= target) {
+  if (c.groups >= target) {
     c.groups_per_block = cdiv(c.groups, target);
     c.parts = 1;
     c.rows_per_part = c.rows_per_group;
@@ -939,7 +963,7 @@ void enqueue_join_backward(const JoinShape &s, const slorr_join_tensors_t &t, co
       q.from[q.kinds++] = i;
     }
   const bool each = a.gate && a.gate_run == 1 && s.gate_rows == s.rows;
-  const int mode = each ? kEachRow : a.gate && c.groups > 1 && c.parts == 1 && s.dim <= 4096 ? kGroups : kOneGate;
+  const int mode = each ? kEachRow : a.gate && c.groups > 1 && c.parts == 1 ? kGroups : kOneGate;
   // kOneGate's blocks leave parts of the gate's sums, to be added afterwards (with no
   // token at all: zeros)
   const bool joined = g.gate && (!s.rows || mode == kOneGate);

@@ -72,6 +72,25 @@ def test_gate_rows_of_many_sequences_without_vectors(kind, dtype):
         _run(dtype, (530, 2, 4104), dtype, given, gate="batch", kind=kind)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("shape", [(257, 2, 4097), (600, 3, 4104), (60, 4, 8192), (3, 2, 5000)])
+def test_gate_rows_of_wide_rows(shape, kind, dtype):
+    """Rows of two pieces per thread under a gate row for each few of them: blocks of one gate row and of several, with
+    dropout and every vector, and with the gate alone; no gradient but the gate's."""
+    import torch
+    from paper_2607_08754_amd import block_join
+    _run(dtype, shape, dtype, VECTORS, gate="batch", scale=True, kind=kind, p=0.2)
+    t, kw, dy, dz = _case(shape, dtype, (), gate="batch", kind=kind)
+    _join_check(t, kw, dy, dz, dtype)
+    full = {k: v for k, v in t.items() if v is not None}
+    y, z = block_join(**full, **kw)
+    want = torch.autograd.grad([y, z], full["gate"], [dy, dz])[0]
+    alone = full["gate"].detach().requires_grad_()
+    y, z = block_join(**{k: alone if k == "gate" else v.detach() for k, v in full.items()}, **kw)
+    assert torch.equal(torch.autograd.grad([y, z], alone, [dy, dz])[0], want)
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("D", [1, 7, 96, 513, 1280, 4097])
 def test_block_norm_without_vectors(D, kind):
