@@ -17,7 +17,8 @@ the current stream of the tensors' device and can be captured into a graph.
 Gradients are formed for the inputs that require them. Each is written anew by
 fixed-order sums: no atomics, so results repeat bit for bit. They can be taken
 once: differentiating them again raises RuntimeError, and so do forward-mode
-derivatives and tracing (torch.jit.trace, make_fx). To capture a
+derivatives and tracing (torch.jit.trace, make_fx); torch.compile ends its graphs
+where they stand. To capture a
 backward() into a graph, let no eager graph of the same leaves live: torch would
 tie the capture to the stream of the older graph.
 
@@ -31,7 +32,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
-from typing import List, Optional, Tuple
+from typing import List, NamedTuple, Optional, Tuple
 
 import torch
 from torch.autograd import forward_ad
@@ -260,16 +261,34 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
 # --------------------------------------------------------------------- join
 
 _JOIN = ("x", "f", "post_weight", "post_bias", "gate", "scale", "pre_weight", "pre_bias")
-_VECTORS = (2, 3, 5, 6, 7)
+_ROWS, _VECTORS = (0, 1, 4), (2, 3, 5, 6, 7)
 
 
-def _join_run(d, shape, tensors, rng):
+class _Call(NamedTuple):
+    """A join without its tensors. (A plain tuple: torch.compile, which splits these functions, loses a ctypes
+    structure's values on the way from one to the next.)"""
+    rows: int
+    dim: int
+    dtype: int
+    norm: int
+    flags: int
+    gate_rows: int
+    eps: float
+    alpha: float
+    p: float
+    site: int
+
+    def struct(self, strides):
+        return _lib.Join(*self[:6], *strides, *self[6:])
+
+
+def _join_run(d: _Call, shape, tensors, strides, rng):
     """The forward call on laid-out inputs: y (None without f) and z (None without PRE)."""
     x = tensors[0]
     with _device(x):
         y = None if tensors[1] is None else _new(shape, x)
         z = _new(shape, x) if d.flags & _lib.JOIN_PRE else None
-        check(lib().slorr_join_forward(d, _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
+        check(lib().slorr_join_forward(d.struct(strides), _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
                                        _stream(x)), "slorr_join_forward")
     return y, z
 
@@ -280,8 +299,8 @@ class _Join(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, d, rng, *tensors):
-        laid = _join_layout(d, tensors)
-        y, z = _join_run(d, tensors[0].shape, laid, rng)
+        laid, strides = _join_layout(d.dim, tensors)
+        y, z = _join_run(d, tensors[0].shape, laid, strides, rng)
         ctx.d = d
         ctx.shapes = [None if t is None else t.shape for t in tensors]
         _save(ctx, rng, *laid)
@@ -294,9 +313,9 @@ class _Join(torch.autograd.Function):
         rng, *laid = _saved(ctx)
         if all(t is None for t in douts):
             return (None,) * (2 + len(laid))
-        d = _lib.Join.from_buffer_copy(ctx.d)
+        d = ctx.d
         with _device(laid[0]):
-            laid = _join_layout(d, laid)
+            laid, strides = _join_layout(d.dim, laid)
             x, rng = laid[0], None if rng is None else _aligned(rng)
             dy = douts[0] if laid[1] is not None else None
             dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
@@ -305,10 +324,10 @@ class _Join(torch.autograd.Function):
             if dz is not None:
                 dz = _aligned(dz)
             grads = [_new(s, t) if n else None for s, t, n in zip(ctx.shapes, laid, ctx.needs_input_grad[2:])]
-            ws = ctypes.c_size_t()
-            check(lib().slorr_join_workspace(d, ws), "slorr_join_workspace")
+            ws, call = ctypes.c_size_t(), d.struct(strides)
+            check(lib().slorr_join_workspace(call, ws), "slorr_join_workspace")
             work = _bytes(ws.value, x)
-            check(lib().slorr_join_backward(d, _lib.JoinTensors(*map(_ptr, laid)), _ptr(rng), _ptr(dy), _ptr(dz),
+            check(lib().slorr_join_backward(call, _lib.JoinTensors(*map(_ptr, laid)), _ptr(rng), _ptr(dy), _ptr(dz),
                                             _lib.JoinTensors(*map(_ptr, grads)), work.data_ptr(), ws.value,
                                             _stream(x)), "slorr_join_backward")
         return (None, None, *grads)
@@ -318,18 +337,16 @@ def _aligned(t: torch.Tensor) -> torch.Tensor:
     return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else _at16(t.contiguous())
 
 
-def _join_layout(d, tensors) -> List[Optional[torch.Tensor]]:
-    """The inputs as the library reads them; the row strides go into d."""
-    out = list(tensors)
-    out[0], d.ldx = _rows(out[0], d.dim)
-    if out[1] is not None:
-        out[1], d.ldf = _rows(out[1], d.dim)
-    if out[4] is not None:
-        out[4], d.ld_gate = _rows(out[4], d.dim)
+def _join_layout(dim, tensors):
+    """The inputs as the library reads them, and the row strides of x, f and gate (0: absent)."""
+    out, strides = list(tensors), [0, 0, 0]
+    for k, i in enumerate(_ROWS):
+        if out[i] is not None:
+            out[i], strides[k] = _rows(out[i], dim)
     for i in _VECTORS:
         if out[i] is not None:
             out[i] = _aligned(out[i])
-    return out
+    return out, strides
 
 
 def _gate_rows(gate: torch.Tensor, x: torch.Tensor) -> int:
@@ -375,17 +392,17 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
     for i in _VECTORS:
         if tensors[i] is not None:
             _check_dense(tensors[i], (dim,), x, _JOIN[i])
-    rows = x.numel() // dim
-    d = _lib.Join(rows, dim, _DTYPE[x.dtype], _NORM[kind], (_lib.JOIN_POST if post else 0) | (_lib.JOIN_PRE if pre else 0),
-                  0, 0, 0, 0, float(eps), float(alpha), float(p), int(site))
+    gate_rows = 0
     if gate is not None:
         if not isinstance(gate, torch.Tensor) or gate.dim() < 1:
             raise ValueError("gate must be a tensor")
         _check_like(gate, (*gate.shape[:-1], dim), x, "gate")
-        d.gate_rows = _gate_rows(gate, x)
+        gate_rows = _gate_rows(gate, x)
+    d = _Call(x.numel() // dim, dim, _DTYPE[x.dtype], _NORM[kind], (_lib.JOIN_POST if post else 0) | (_lib.JOIN_PRE if pre else 0),
+              gate_rows, float(eps), float(alpha), float(p), int(site))
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         return _Join.apply(d, rng, *tensors)
-    y, z = _join_run(d, x.shape, _join_layout(d, tensors), rng)
+    y, z = _join_run(d, x.shape, *_join_layout(dim, tensors), rng)
     return (y, z) if y is not None and z is not None else z if y is None else y
 
 

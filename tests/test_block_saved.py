@@ -98,11 +98,10 @@ def join_pass(lib):
     x, f = (torch.randn(6, 40)[:, :D].requires_grad_() for _ in range(2))
     gate = torch.randn(3, 64)[:, :D].requires_grad_()
     v = [torch.randn(D).requires_grad_() for _ in range(5)]
-    d = _lib.Join(6, D, _lib.F32, _lib.LAYER, _lib.JOIN_POST | _lib.JOIN_PRE, 3, 0, 0, 0, 1e-5, 1.0, 0.5, 0)
+    d = block._Call(6, D, _lib.F32, _lib.LAYER, _lib.JOIN_POST | _lib.JOIN_PRE, 3, 1e-5, 1.0, 0.5, 0)
     rng = torch.zeros(2, dtype=torch.int64)
     y, z = block._Join.apply(d, rng, x, f, v[0], v[1], gate, v[2], v[3], v[4])
     torch.autograd.grad([y, z], [x, f, gate, *v], [torch.ones_like(y)] * 2)
-    assert (d.ldx, d.ldf, d.ld_gate) == (40, 40, 64)       # the forward call's own
 
 
 def dropout_pass(lib):
@@ -163,6 +162,6 @@ def test_tensors_without_memory_are_refused(lib):
     x = torch.randn(6, 16)
     v = torch.randn(16)
     v.untyped_storage().resize_(0)
-    d = _lib.Join(6, 16, _lib.F32, _lib.LAYER, _lib.JOIN_PRE, 0, 0, 0, 0, 1e-5, 1.0, 0.0, 0)
+    d = block._Call(6, 16, _lib.F32, _lib.LAYER, _lib.JOIN_PRE, 0, 1e-5, 1.0, 0.0, 0)
     with pytest.raises(ValueError, match="no memory"):
-        block._join_run(d, x.shape, block._join_layout(d, (x, None, None, None, None, None, v, None)), None)
+        block._join_run(d, x.shape, *block._join_layout(16, (x, None, None, None, None, None, v, None)), None)
