@@ -32,6 +32,8 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
+import struct
+import weakref
 from typing import List, NamedTuple, Optional, Tuple
 
 import torch
@@ -148,20 +150,17 @@ def _ptr(t: Optional[torch.Tensor]):
     return p
 
 
-def _save(ctx, *tensors) -> None:
-    ctx.save_for_backward(*tensors)
-    ctx.kinds = [None if t is None else (t.shape, t.dtype, t.device) for t in tensors]
+def _returned(t: torch.Tensor, shape, dtype: torch.dtype, device: int) -> torch.Tensor:
+    """A saved tensor as it comes back. saved_tensors_hooks may return another one, at another address and in
+    another layout: the backward calls lay the tensors out again. Anything else about it has to be as it was."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise RuntimeError(f"a saved tensor of {dtype} {tuple(shape)} came back as {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
 
 
-def _saved(ctx):
-    """The saved tensors. saved_tensors_hooks may return them at other addresses and
-    in other layouts, so the backward calls lay them out again; anything else about
-    them has to be as it was."""
-    tensors = ctx.saved_tensors
-    for t, kind in zip(tensors, ctx.kinds):
-        if kind is not None and (t.shape, t.dtype, t.device) != kind:
-            raise RuntimeError(f"a saved tensor of {kind[1]} {tuple(kind[0])} on {kind[2]} came back as {t.dtype} {tuple(t.shape)} on {t.device}")
-    return tensors
+def _returned_dense(t: Optional[torch.Tensor], *of) -> Optional[torch.Tensor]:
+    """The same of a tensor that is read as contiguous (None: none was saved)."""
+    return None if t is None else _aligned(_returned(t, *of))
 
 
 def _bytes(n: int, like: torch.Tensor) -> torch.Tensor:
@@ -206,19 +205,21 @@ class _GatedFfn(torch.autograd.Function):
     def forward(ctx, x, w_gate, w_up, w_down, act):
         rows, ldx = _rows(x, w_gate.shape[1])
         y, state = _ffn_forward(rows, x.shape, ldx, w_gate, w_up, w_down, act, True)
-        ctx.act, ctx.shape = act, x.shape
-        _save(ctx, rows, w_gate, w_up, w_down, state)
+        ctx.act, ctx.shape, ctx.laid, ctx.inner, ctx.state_bytes = act, x.shape, rows.shape, w_gate.shape[0], state.shape
+        ctx.save_for_backward(rows, w_gate, w_up, w_down, state)
         return y
 
     @staticmethod
     @_once
     def backward(ctx, dy):
-        x, w_gate, w_up, w_down, state = _saved(ctx)
-        need = ctx.needs_input_grad
-        with _device(x):
-            x, ldx = _rows(x, w_gate.shape[1])
-            w_gate, w_up, w_down, state = _aligned(w_gate), _aligned(w_up), _aligned(w_down), _aligned(state)
-            dy, lddy = _rows(dy, w_gate.shape[1])
+        x, w_gate, w_up, w_down, state = ctx.saved_tensors
+        need, dim, inner, of = ctx.needs_input_grad, ctx.shape[-1], ctx.inner, (dy.dtype, dy.get_device())
+        with _device(dy):
+            x, ldx = _rows(_returned(x, ctx.laid, *of), dim)
+            w_gate, w_up = _returned_dense(w_gate, (inner, dim), *of), _returned_dense(w_up, (inner, dim), *of)
+            w_down = _returned_dense(w_down, (dim, inner), *of)
+            state = _returned_dense(state, ctx.state_bytes, torch.uint8, of[1])
+            dy, lddy = _rows(dy, dim)
             d = _ffn_block(x, ldx, w_gate, ctx.act, lddy)
             ws = ctypes.c_size_t()
             check(lib().slorr_ffn_sizes(d, None, None, ws), "slorr_ffn_sizes")
@@ -279,18 +280,22 @@ class _Call(NamedTuple):
     site: int
 
     def struct(self, strides):
-        return _lib.Join(*self[:6], *strides, *self[6:])
+        return _lib.Join.from_buffer_copy(_PACKED.pack(*self[:6], *strides, *self[6:]))
+
+
+_PACKED = struct.Struct("@qiiiIqqqqffdq")           # _lib.Join: packed at half of what its constructor takes
+assert _PACKED.size == ctypes.sizeof(_lib.Join)
 
 
 def _join_run(d: _Call, shape, tensors, strides, rng):
-    """The forward call on laid-out inputs: y (None without f) and z (None without PRE)."""
-    x = tensors[0]
+    """The forward call on laid-out inputs: y (None without f), z (None without PRE) and the inputs' addresses."""
+    x, at = tensors[0], [*map(_ptr, tensors)]
     with _device(x):
         y = None if tensors[1] is None else _new(shape, x)
         z = _new(shape, x) if d.flags & _lib.JOIN_PRE else None
-        check(lib().slorr_join_forward(d.struct(strides), _lib.JoinTensors(*map(_ptr, tensors)), _ptr(rng), _ptr(y), _ptr(z),
+        check(lib().slorr_join_forward(d.struct(strides), _lib.JoinTensors(*at), _ptr(rng), _ptr(y), _ptr(z),
                                        _stream(x)), "slorr_join_forward")
-    return y, z
+    return y, z, at
 
 
 class _Join(torch.autograd.Function):
@@ -300,34 +305,52 @@ class _Join(torch.autograd.Function):
     @staticmethod
     def forward(ctx, d, rng, *tensors):
         laid, strides = _join_layout(d.dim, tensors)
-        y, z = _join_run(d, tensors[0].shape, laid, strides, rng)
-        ctx.d = d
-        ctx.shapes = [None if t is None else t.shape for t in tensors]
-        _save(ctx, rng, *laid)
+        y, z, at = _join_run(d, tensors[0].shape, laid, strides, rng)
+        ctx.d, ctx.strides, ctx.at = d, strides, at
+        ctx.refs = [None if t is None else weakref.ref(t) for t in (rng, *laid)]
+        ctx.shapes = [None if tensors[i] is None else tensors[i].shape for i in _ROWS]
+        ctx.save_for_backward(rng, *laid)
         ctx.set_materialize_grads(False)
         return (y, z) if y is not None and z is not None else z if y is None else y
 
     @staticmethod
     @_once
     def backward(ctx, *douts):
-        rng, *laid = _saved(ctx)
-        if all(t is None for t in douts):
+        rng, *laid = ctx.saved_tensors
+        d, some = ctx.d, douts[0] if douts[0] is not None else douts[-1]
+        if some is None:
             return (None,) * (2 + len(laid))
-        d = ctx.d
-        with _device(laid[0]):
-            laid, strides = _join_layout(d.dim, laid)
-            x, rng = laid[0], None if rng is None else _aligned(rng)
+        of = (some.dtype, some.get_device())
+        with _device(some):
+            strides, at = ctx.strides, [*map(_ptr, laid)]
+            if at != ctx.at or not all(t is None or r() is t for r, t in zip(ctx.refs, (rng, *laid))):
+                # not the tensors that were saved (checks and strides that cost a call 8 us)
+                for i, shape in zip(_ROWS, ctx.shapes):
+                    if laid[i] is not None:
+                        _returned(laid[i], shape if laid[i].shape == shape else (shape.numel() // d.dim, d.dim), *of)
+                for i in _VECTORS:
+                    laid[i] = _returned_dense(laid[i], (d.dim,), *of)
+                rng = _returned_dense(rng, (2,), torch.int64, of[1])
+                laid, strides = _join_layout(d.dim, laid)
+                at = [*map(_ptr, laid)]
+            x = laid[0]
             dy = douts[0] if laid[1] is not None else None
             dz = douts[-1] if d.flags & _lib.JOIN_PRE else None
             if dy is not None:
                 dy = _aligned(dy)
             if dz is not None:
                 dz = _aligned(dz)
-            grads = [_new(s, t) if n else None for s, t, n in zip(ctx.shapes, laid, ctx.needs_input_grad[2:])]
+            need, grads = ctx.needs_input_grad[2:], [None] * len(laid)
+            for i in _VECTORS:
+                if need[i]:
+                    grads[i] = torch.empty_like(laid[i])
+            for i, shape in zip(_ROWS, ctx.shapes):
+                if need[i]:
+                    grads[i] = _new(shape, laid[i])
             ws, call = ctypes.c_size_t(), d.struct(strides)
             check(lib().slorr_join_workspace(call, ws), "slorr_join_workspace")
             work = _bytes(ws.value, x)
-            check(lib().slorr_join_backward(call, _lib.JoinTensors(*map(_ptr, laid)), _ptr(rng), _ptr(dy), _ptr(dz),
+            check(lib().slorr_join_backward(call, _lib.JoinTensors(*at), _ptr(rng), _ptr(dy), _ptr(dz),
                                             _lib.JoinTensors(*map(_ptr, grads)), work.data_ptr(), ws.value,
                                             _stream(x)), "slorr_join_backward")
         return (None, None, *grads)
@@ -345,7 +368,7 @@ def _join_layout(dim, tensors):
             out[i], strides[k] = _rows(out[i], dim)
     for i in _VECTORS:
         if out[i] is not None:
-            out[i] = _aligned(out[i])
+            out[i] = _at16(out[i])
     return out, strides
 
 
@@ -402,7 +425,7 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
               gate_rows, float(eps), float(alpha), float(p), int(site))
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         return _Join.apply(d, rng, *tensors)
-    y, z = _join_run(d, x.shape, *_join_layout(dim, tensors), rng)
+    y, z, _ = _join_run(d, x.shape, *_join_layout(dim, tensors), rng)
     return (y, z) if y is not None and z is not None else z if y is None else y
 
 
@@ -462,14 +485,14 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, p, rng, site):
         ctx.p, ctx.site = p, site
-        _save(ctx, rng)
+        ctx.save_for_backward(rng)
         return _dropout_run(x, p, rng, site)
 
     @staticmethod
     @_once
     def backward(ctx, dy):
-        rng, = _saved(ctx)
-        return _dropout_run(dy, ctx.p, None if rng is None else _aligned(rng), ctx.site), None, None, None
+        rng = _returned_dense(ctx.saved_tensors[0], (2,), torch.int64, dy.get_device())
+        return _dropout_run(dy, ctx.p, rng, ctx.site), None, None, None
 
 
 def dropout(x: torch.Tensor, p: float, rng: Optional[torch.Tensor], site: int = 0) -> torch.Tensor:

