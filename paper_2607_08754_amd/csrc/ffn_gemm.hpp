@@ -650,11 +650,13 @@ __global__ __launch_bounds__(256) void k_tail(FfnArgs args) {
 // (lane l: row l % 16, k from 8 (l / 16) on; fp32: four k of 4 (l / 16) on in
 // four instructions), the tokens are the other operand, read through the caches
 // by every block. The waves' sums meet in LDS. No row alignment is needed. One token
-// of 1536 x 6144 in bf16: 38 MB of Wg and Wu in 10.8 us, 19 MB of Wd in 8.9 (the
-// copy's rate would take 7.7 and 3.9; the rest is the start of a launch, one trip to
-// HBM and the sums' way through LDS). The tiles of k_ffn take 33 us for both. Not
-// kept: chunks loaded one to three ahead (19.0 against 18.6 us), blocks that begin at
-// different chunks (no change).
+// of 1536 x 6144 in bf16: 38 MB of Wg and Wu in 11.1 us, 19 MB of Wd in 9.1, where the
+// copy's rate would take 7.7 and 3.9. Blocks bound it where there are fewer than CUs: 384
+// read Wg and Wu, but 96 read Wd, and 160 of the 256 CUs read nothing meanwhile (7 tokens
+// of 768 x 2048 in fp32: 128 and 48 blocks, 7.7 and 8.1 us). The rest is the start of a
+// launch, one trip to HBM and the sums' way through LDS. The tiles of k_ffn take 33 us for
+// both launches. Not kept: chunks loaded one to three ahead (19.0 against 18.6 us), blocks
+// that begin at different chunks (no change).
 struct FewArgs {
   const void *x, *w0, *w1;
   void *out;                   // h or y

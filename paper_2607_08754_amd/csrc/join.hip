@@ -308,10 +308,12 @@ __device__ __forceinline__ void products(const JoinArgs &a, const T *gate, Row<N
 // A block takes a run of rows, each thread NV pieces of 8 columns of a row; the
 // next row's loads are issued before the current row's sums, and the vectors'
 // products are formed once per gate row. WHOLE: rows of whole pieces; the code for
-// a row's end, which is there for every tensor, costs 16384 x 1280 bf16 3 of 35 us
-// (backward 23 of 92) even where no row has one. HBM bounds the kernel (168 MB in 28 us, 6.0
-// TB/s) up to the generator, whose 20 32 x 32 products and 40 other instructions
-// per 8 elements add 3.7 us.
+// a row's end, which is there for every tensor, costs 16384 x 1280 bf16 4 of 49 us
+// (backward 25 of 91) even where no row has one. In a training pass that shape takes 44
+// us, 168 MB at 3.8 TB/s with the waves waiting 67 % of their time: bound by HBM and by a
+// row's chain of sums. Called again and again on the same inputs, which the memory-side
+// cache then holds, it takes 32 us. The generator, 20 32 x 32 products and 40 other
+// instructions per 8 elements, is 3.5 us of either.
 template <typename T, int NV, bool BIAS, bool WHOLE>
 __global__ __launch_bounds__(512) void k_join_fwd(JoinArgs a) {
   __shared__ RowSums sh;
@@ -404,7 +406,7 @@ enum GateMode { kOneGate = 0, kEachRow = 1, kGroups = 2, kRuns = 3 };
 // A row has three block sums one after the other (RMS; LAYER five): the next
 // row is loaded before them, and the y norm's two sums share one.
 //
-// 16384 x 1280 in bf16 with both norms, gate, scale and dropout: 69 us, 252 MB of
+// 16384 x 1280 in bf16 with both norms, gate, scale and dropout: 68 us, 252 MB of
 // tensors and 39 MB of partial rows at 4.2 TB/s; VALU busy half of the time, waves
 // waiting 63 % of theirs: bound by a row's chain of sums as much as by HBM.
 template <typename T, int NV, int MODE, bool BIAS, bool WHOLE>
@@ -893,9 +895,10 @@ void launch_backward(const JoinArgs &a, int mode, int64_t blocks, hipStream_t st
 JoinCut join_cut(const JoinShape &s) {
   JoinCut c;
   // as many blocks as the CUs hold at once, by the kernels' registers: 16 waves per
-  // CU with bf16 rows of one piece per thread, else 8 (us with 4 blocks per CU
-  // whatever their size, and so: 65536 x 512 bf16 232, 123; 4096 x 4096 bf16 84, 65;
-  // 4096 x 6144 bf16 182, 151; 8192 x 4096 fp32 260, 224; 16384 x 1280 bf16 112, 109)
+  // CU with bf16 rows of one piece per thread, else 8 (us of k_join_bwd and k_join_sum
+  // with 4 blocks per CU whatever their size, and so: 65536 x 512 bf16 189, 113; 4096 x
+  // 4096 bf16 75, 59; 4096 x 6144 bf16 189, 144; 8192 x 4096 fp32 224, 197; 16384 x 1280
+  // bf16 77, 74)
   const int waves = s.dim <= 4096 && s.dtype == SLORR_BF16 ? 16 : 8;
   const int64_t target = int64_t(kCus) * std::max(1, waves * 64 / join_threads(s.dim));
   const bool summed = s.gate_rows > 1 && s.gate_rows < s.rows;     // gate rows of several tokens each
@@ -929,8 +932,10 @@ void enqueue_join_forward(const JoinShape &s, const slorr_join_tensors_t &t, con
   a.y = y;
   a.z = z;
   // as many blocks as the CUs hold at once, each a run of rows: 16 waves per CU, 24
-  // where the registers allow it (16384 x 1280 bf16: 36.6 us with 16, 31.6 with 24;
-  // 4096 x 6144 bf16, whose blocks are 8 waves: 53 us with 8, 41 with 16)
+  // where the registers allow it (us with 16 and 24: 65536 x 512 bf16 in a training pass
+  // 69.5, 53.6; 16384 x 1280 bf16 41.7, 44.2, and called again on inputs that the
+  // memory-side cache holds 37.0, 32.1; 4096 x 2048 bf16 17.0, 16.8. 4096 x 6144 bf16,
+  // whose blocks are 8 waves: 60 with 8, 49.5 with 16)
   const int threads = join_threads(s.dim);
   const int waves = s.dim <= 4096 && s.dtype == SLORR_BF16 && !a.b1 && !a.b2 ? 24 : 16;
   a.per_block = std::max<int64_t>(1, cdiv(s.rows, kCus * (waves * 64 / threads)));
