@@ -31,7 +31,6 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
-import math
 import struct
 import weakref
 from typing import List, NamedTuple, Optional, Tuple
@@ -49,6 +48,7 @@ _ACT = {"silu": _lib.SILU, "gelu": _lib.GELU, "gelu_tanh": _lib.GELU_TANH}
 _NORM = {"rms": _lib.RMS, "layer": _lib.LAYER}
 _MAX_STRIDE = (1 << 22) - 8
 _MAX_NORM = 8192
+_MOST_F32 = (2.0 - 2.0 ** -23) * 2.0 ** 127
 _MOST_P = (65535.5 - 2.0 ** -20) / 65536          # p counts in steps of 2^-16
 
 
@@ -61,7 +61,7 @@ def _check_transforms(*tensors) -> None:
     would be lost, and traces, which would hold the outputs' allocation alone."""
     if _is_tracing() or (_modes() and torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None):
         raise RuntimeError("the block operators cannot be traced (a captured graph holds them)")
-    if forward_ad._current_level >= 0:
+    if getattr(forward_ad, "_current_level", 0) >= 0:
         for t in tensors:
             if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
                 raise RuntimeError("the block operators have no forward-mode derivative")
@@ -408,8 +408,8 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
     dim, gate = x.shape[-1], tensors[4]
     if dim > _MAX_NORM:
         raise ValueError(f"the last dimension must be at most {_MAX_NORM}")
-    if not (0.0 <= eps < math.inf and math.isfinite(alpha)):
-        raise ValueError("eps must be >= 0, eps and alpha finite")
+    if not (0.0 <= eps <= _MOST_F32 and abs(alpha) <= _MOST_F32):
+        raise ValueError("eps must be >= 0, eps and alpha finite in float32")
     if f is not None:
         _check_like(f, x.shape, x, "f")
     for i in _VECTORS:
@@ -422,7 +422,7 @@ def _join_call(x, f, kind, eps, post, pre, tensors, alpha, p, rng, site):
         _check_like(gate, (*gate.shape[:-1], dim), x, "gate")
         gate_rows = _gate_rows(gate, x)
     d = _Call(x.numel() // dim, dim, _DTYPE[x.dtype], _NORM[kind], (_lib.JOIN_POST if post else 0) | (_lib.JOIN_PRE if pre else 0),
-              gate_rows, float(eps), float(alpha), float(p), int(site))
+              gate_rows, float(eps), float(alpha), float(p), ctypes.c_int64(int(site)).value)      # (site: modulo 2^64)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         return _Join.apply(d, rng, *tensors)
     y, z, _ = _join_run(d, x.shape, *_join_layout(dim, tensors), rng)

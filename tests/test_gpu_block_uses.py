@@ -80,3 +80,21 @@ def test_inside_a_compiled_function():
     a, b = f(x), compiled(x)
     for s, t in zip([a, *torch.autograd.grad(a, leaves, dy)], [b, *torch.autograd.grad(b, leaves, dy)]):
         assert torch.equal(s, t)
+
+
+def test_sites_of_any_size_and_factors_past_float32():
+    """Sites count modulo 2^64, as the generator's offset does; a factor that float32 does not hold is refused."""
+    import torch
+    from paper_2607_08754_amd import block_join, block_norm, dropout
+    x, f = _tensor((5, 40), "f32", 1), _tensor((5, 40), "f32", 2)
+    rng = torch.tensor([9, 100], dtype=torch.int64, device=DEV)
+    for fn in (lambda s: dropout(x, 0.5, rng, site=s), lambda s: block_join(x, f, p=0.5, rng=rng, site=s)[0]):
+        want = fn(5)
+        assert torch.equal(fn(5 + 2 ** 64), want) and torch.equal(fn(5 - 2 ** 64), want)
+        assert torch.equal(fn(2 ** 63), fn(-2 ** 63)) and not torch.equal(fn(2 ** 63), want)
+    for kw in (dict(alpha=1e39), dict(alpha=-1e300), dict(eps=1e39)):
+        with pytest.raises(ValueError, match="eps must"):
+            block_join(x, f, **kw)
+    with pytest.raises(ValueError, match="eps must"):
+        block_norm(x, eps=1e300)
+    assert torch.isfinite(block_join(x, f, alpha=1e30)[0]).all()
